@@ -8,7 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = [os.path.join(CSRC, f) for f in ("dtr_sim.cpp", "dtr_log.cpp", "replay.hip", "replay_log.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("dtr_sim.cpp", "dtr_log.cpp", "replay.hip", "replay_log.hip",
+                                            "dtr_ops.cpp", "attention.hip", "rows.hip")]
 OUT = os.path.join(HERE, "libdtrsim.so")
 # the same sources with the in-kernel cycle timers (profile.py); never the product
 OUT_PROFILE = os.path.join(HERE, "libdtrsim_prof.so")

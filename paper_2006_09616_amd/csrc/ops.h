@@ -1,0 +1,72 @@
+// ops.h -- what the host file (dtr_ops.cpp) and the kernels of the operators
+// (attention.hip, rows.hip) share: argument records, launch plans and the
+// launchers.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+namespace dtrops {
+
+constexpr int KEY_TILE = 64;      // keys of a tile of the attention kernels
+constexpr int ROW_TILE = 128;     // rows (queries x heads of a group) of a workgroup
+constexpr int SEGS = 4;           // segments of a row that a workgroup of the log-probability kernel reads
+
+struct Heads {                    // [batch][position][head][head_dim], strides in elements
+    char *data;
+    int64_t batch, position, head;
+};
+
+struct AttnArgs {
+    int32_t batch, q_len, k_len, k_heads, group, head_dim, causal;
+    float scale, cap;
+    const float *slopes;
+    const int32_t *prefix, *docs, *lengths, *starts;
+    Heads q, k, v, out, dout, dq, dk, dv;
+    float *lse;                   // [batch][q_heads][q_len]
+    int32_t rows;                 // q_len * group: rows of one key head, row = query * group + head of the group
+    int32_t splits;               // parts that the keys are split into (forward)
+    int32_t key_tiles;            // ceil(k_len / KEY_TILE)
+    int2 *doc_tiles;              // [batch][key_tiles] smallest and largest document of each tile
+    float *part_out;              // [splits][batch][k_heads][rows][head_dim] (splits > 1)
+    float2 *part_stat;            // [splits][batch][k_heads][rows] maximum and sum
+    float2 *row_stat;             // [batch][k_heads][rows] log2-sum-exp2 and out.dout (backward)
+};
+
+struct LogpArgs {
+    int64_t rows, vocab, stride;
+    int32_t top, splits;
+    const void *x;
+    const int64_t *tokens;
+    float *logp, *entropy, *lse, *top_logp;
+    int64_t *top_ids;
+    float *part;                  // [rows][segments][4] maximum, sum, weighted sum, entries
+    float2 *part_top;             // [rows][segments][top] value, column (as bits)
+};
+
+struct LogpGradArgs {
+    int64_t rows, vocab, stride, dstride;
+    int32_t top;
+    const void *x;
+    const int64_t *tokens, *top_ids;
+    const float *entropy, *lse, *dlogp, *dentropy, *dtop;
+    void *dx;
+};
+
+struct DropArgs {
+    int64_t rows, cols, x_stride, r_stride, o_stride;
+    const void *x, *residual;
+    void *out;
+    uint64_t key, offset, threshold;
+    float inv;
+    int32_t vector;               // groups of 8 elements start at multiples of 16 bytes
+};
+
+hipError_t launch_attn_forward(const AttnArgs &a, int type, hipStream_t st);
+hipError_t launch_attn_backward(const AttnArgs &a, int type, hipStream_t st);
+hipError_t launch_logprobs(const LogpArgs &a, int type, hipStream_t st);
+hipError_t launch_logprobs_grad(const LogpGradArgs &a, int type, hipStream_t st);
+hipError_t launch_dropout(const DropArgs &a, int type, hipStream_t st);
+
+}  // namespace dtrops

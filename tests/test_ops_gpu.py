@@ -1,0 +1,693 @@
+"""The operators on the GPU against their definitions in 64 bits.
+
+Tolerances are bounds, element by element, derived from what the kernels
+round: u is the unit roundoff of the tensors' type (2^-8 bf16, 2^-11 fp16,
+2^-24 fp32), every sum and statistic is held in 32 bits, and probabilities and
+score gradients are rounded to the tensors' type once, before a product."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+TINY = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -25, torch.float32: 0.0}       # half the smallest fp16 step
+BF, FP, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2006_09616_amd import ops as O
+    O.lib()
+    return O
+
+
+# ---- attention --------------------------------------------------------------------
+
+def definition(q, k, v, do, scale, cap, slopes, causal, prefix, docs, lengths, starts):
+    """out, lse, dq, dk, dv in 64 bits and, for each, the bound of what the
+    kernels' roundings come to."""
+    u, tiny = U[q.dtype], TINY[q.dtype]
+    q, k, v, do = (t.detach().double().cpu() for t in (q, k, v, do))
+    B, Sq, Hq, D = q.shape
+    Sk, Hk = k.shape[1], k.shape[2]
+    res = {n: torch.zeros_like(t) for n, t in (("out", q), ("dq", q), ("dk", k), ("dv", v))}
+    tol = {n: torch.zeros_like(t) for n, t in res.items()}
+    res["lse"] = torch.full((B, Hq, Sq), -math.inf, dtype=torch.float64)
+    tol["lse"] = torch.zeros(B, Hq, Sq, dtype=torch.float64)
+    j = torch.arange(Sk)[None]
+    for b in range(B):
+        p = (torch.arange(Sq) + (int(starts[b]) if starts is not None else Sk - Sq))[:, None]
+        seen = (j < (int(lengths[b]) if lengths is not None else Sk)).expand(Sq, Sk).clone()
+        if causal:
+            seen &= (j <= p) | (j < (int(prefix[b]) if prefix is not None else 0))
+        if docs is not None:
+            d = docs[b].cpu()
+            inside = (p >= 0) & (p < Sk)
+            seen &= inside & (d[p.clamp(0, max(Sk - 1, 0))] == d[None])
+        for h in range(Hq):
+            Q, G = q[b, :, h], do[b, :, h]
+            K, V = k[b, :, h // (Hq // Hk)].clone(), v[b, :, h // (Hq // Hk)].clone()
+            unseen = ~seen.any(0)
+            K[unseen] = 0                                 # values that no query sees may be anything
+            V[unseen] = 0
+            r = scale * Q @ K.T
+            mag = scale * Q.abs() @ K.abs().T
+            s, dc = r, torch.ones_like(r)
+            if cap:
+                t = torch.tanh(r / cap)
+                s, dc = cap * t, 1 - t * t
+            dist = (p - j).abs().double()
+            sl = float(slopes[h]) if slopes is not None else 0.0
+            s = (s - sl * dist).masked_fill(~seen, -math.inf)
+            L = torch.logsumexp(s, 1, keepdim=True) if Sk else torch.full((Sq, 1), -math.inf, dtype=torch.float64)
+            empty = ~seen.any(1, keepdim=True)
+            P = torch.where(seen, torch.exp(s - L), 0.0)
+            # relative error of a probability that 32-bit scores and statistics leave: the product's sum
+            # over D, tanh and exp2 to a few units of 2^-24, and the sum over Sk
+            e = (2.0 ** -20 * (1 + mag) + cap * 2.0 ** -20 + sl * dist * 2.0 ** -22 + 2.0 ** -24 * s.abs().nan_to_num(0, 0, 0) * 8)
+            e = torch.where(seen, e, 0.0)
+            e = e + (P * e).sum(1, keepdim=True) + 2.0 ** -22 * math.sqrt(Sk + 1)
+            out = P @ V
+            # p is rounded relative to the running maximum, so that P = 1 is at least 2^-25 of it away
+            et = u * P + e * P + tiny * seen
+            t_out = et @ V.abs() + u * out.abs() + tiny
+            g = h // (Hq // Hk)
+            res["out"][b, :, h], tol["out"][b, :, h] = out, t_out
+            res["lse"][b, h] = L[:, 0]
+            tol["lse"][b, h] = torch.where(empty[:, 0], 0.0, (P * e).sum(1) + 2.0 ** -20 * (1 + L[:, 0].abs().nan_to_num(0, 0, 0)))
+            dP = G @ V.T
+            Dl = (G * out).sum(1, keepdim=True)
+            dS = P * (dP - Dl)
+            t_D = (G.abs() * t_out).sum(1, keepdim=True) + 2.0 ** -21 * (G * out).abs().sum(1, keepdim=True)
+            t_dS = (u + e) * dS.abs() + P * (t_D + 2.0 ** -20 * (G.abs() @ V.abs().T)) + tiny * seen
+            if cap:
+                t_dS = t_dS * dc + dS.abs() * 2.0 ** -19 * (1 + mag / cap)
+                dS = dS * dc
+            t_P = (u + e) * P + tiny * seen
+            res["dq"][b, :, h] = scale * dS @ K
+            tol["dq"][b, :, h] = scale * t_dS @ K.abs() + u * res["dq"][b, :, h].abs() + tiny
+            res["dk"][b, :, g] += scale * dS.T @ Q
+            tol["dk"][b, :, g] += scale * t_dS.T @ Q.abs()
+            res["dv"][b, :, g] += P.T @ G
+            tol["dv"][b, :, g] += t_P.T @ G.abs()
+    for n in ("dk", "dv"):
+        tol[n] += u * res[n].abs() + tiny
+    return res, tol
+
+
+def close(got, want, tol, label):
+    got = got.detach().double().cpu()
+    assert got.shape == want.shape, label
+    inf = torch.isinf(want)
+    assert torch.equal(got[inf], want[inf]), f"{label}: infinities differ"
+    bad = ~((got - want).abs() <= tol) & ~inf
+    if bad.any():
+        i = tuple(int(x) for x in bad.nonzero()[0])
+        raise AssertionError(f"{label}: {int(bad.sum())} of {bad.numel()} off, first {i}: {float(got[i])} for "
+                             f"{float(want[i])} +- {float(tol[i])}")
+
+
+def inputs(B, Sq, Sk, Hq, Hk, D, dtype, layout="separate", seed=0, gain=1.0):
+    g = torch.Generator().manual_seed(seed * 7919 + Sq * 131 + Sk * 17 + D)
+
+    def normal(*shape, a=1.0):
+        return (torch.randn(*shape, generator=g) * a).to(dtype).cuda()
+
+    if layout == "packed":
+        x = normal(B, Sq, Hq + 2 * Hk, D)
+        q, k, v = x[:, :, :Hq], x[:, :, Hq:Hq + Hk], x[:, :, Hq + Hk:]
+    elif layout == "heads":
+        q, k, v = (normal(B, h, s, D).transpose(1, 2) for h, s in ((Hq, Sq), (Hk, Sk), (Hk, Sk)))
+    elif layout == "offset":                             # rows at odd multiples of 2 bytes: copied
+        q, k, v = (normal(B, s, h, D + 3)[..., 1:D + 1] for h, s in ((Hq, Sq), (Hk, Sk), (Hk, Sk)))
+    elif layout == "time":                               # [S, B, H, D]
+        q, k, v = (normal(s, B, h, D).transpose(0, 1) for h, s in ((Hq, Sq), (Hk, Sk), (Hk, Sk)))
+    else:
+        q, k, v = normal(B, Sq, Hq, D), normal(B, Sk, Hk, D), normal(B, Sk, Hk, D)
+    q, k, v = (t.detach().requires_grad_() for t in (q * gain if gain != 1.0 else q, k, v))
+    return q, k, v, normal(B, Sq, Hq, D, a=0.25)
+
+
+def check(ops, q, k, v, do, label, scale=None, cap=0.0, slopes=None, causal=False, prefix=None, docs=None, lengths=None,
+          starts=None, backward=True):
+    print(label, flush=True)
+    scale_ = scale if scale is not None else q.shape[3] ** -0.5
+    dev = [t.cuda() if t is not None else None for t in (slopes, prefix, docs, lengths, starts)]
+    kw = dict(scale=scale, cap=cap, slopes=dev[0], causal=causal, prefix=dev[1], docs=dev[2], lengths=dev[3], starts=dev[4])
+    want, tol = definition(q, k, v, do, scale_, cap, slopes, causal, prefix, docs, lengths, starts)
+    if not backward:
+        with torch.no_grad():
+            out, lse = ops.attention(q, k, v, return_lse=True, **kw)
+        close(out, want["out"], tol["out"], label + " out")
+        close(lse, want["lse"], tol["lse"], label + " lse")
+        return
+    out, lse = ops.attention(q, k, v, return_lse=True, **kw)
+    close(out, want["out"], tol["out"], label + " out")
+    close(lse, want["lse"], tol["lse"], label + " lse")
+    grads = torch.autograd.grad(out, (q, k, v), do)
+    for n, t in zip(("dq", "dk", "dv"), grads):
+        close(t, want[n], tol[n], f"{label} {n}")
+
+
+LENGTHS = [(1, 1), (1, 2), (2, 1), (3, 5), (31, 31), (32, 33), (33, 32), (64, 64), (65, 63), (127, 129), (128, 128),
+           (130, 257), (200, 77)]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_lengths(ops, dtype, causal):
+    for i, (Sq, Sk) in enumerate(LENGTHS):
+        q, k, v, do = inputs(2, Sq, Sk, 4, 2, 64, dtype, seed=i)
+        check(ops, q, k, v, do, f"{dtype} causal {causal} {Sq} {Sk}", causal=causal)
+
+
+@pytest.mark.parametrize("D", [8, 16, 24, 40, 56, 64, 72, 80, 96, 104, 128])
+def test_attention_head_sizes(ops, D):
+    for i, (dtype, cap) in enumerate(((BF, 0.0), (FP, 5.0))):
+        q, k, v, do = inputs(1, 70, 70, 3, 1, D, dtype, seed=i, gain=2.0)
+        check(ops, q, k, v, do, f"head size {D} {dtype}", cap=cap, causal=True, slopes=torch.tensor([0.5, 0.1, 0.0]))
+
+
+@pytest.mark.parametrize("heads", [(1, 1), (2, 1), (6, 2), (5, 5), (8, 1), (48, 1)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_grouped_heads(ops, heads, D):
+    Hq, Hk = heads
+    q, k, v, do = inputs(2, 37, 90, Hq, Hk, D, BF, seed=Hq)
+    check(ops, q, k, v, do, f"heads {heads} {D}", causal=True, cap=20.0)
+
+
+@pytest.mark.parametrize("layout", ["packed", "heads", "offset", "time"])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_attention_layouts(ops, layout, dtype):
+    q, k, v, do = inputs(3, 75, 75, 4, 2, 64, dtype, layout)
+    check(ops, q, k, v, do, f"layout {layout}", causal=True)
+    # the output's gradient in an order of its own
+    do = do.permute(2, 0, 1, 3).contiguous().permute(1, 2, 0, 3)
+    check(ops, q, k, v, do, f"layout {layout}, gradient by heads", causal=False)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 3.0, 50.0])
+@pytest.mark.parametrize("bias", [False, True])
+def test_attention_scores(ops, D, cap, bias):
+    slopes = torch.tensor([1.0, 0.25, 0.01, 0.0]) if bias else None
+    for causal in (False, True):
+        q, k, v, do = inputs(1, 150, 150, 4, 2, D, BF, gain=4.0, seed=int(cap))
+        check(ops, q, k, v, do, f"cap {cap} bias {bias} causal {causal} {D}", cap=cap, slopes=slopes, causal=causal)
+    q, k, v, do = inputs(1, 40, 190, 4, 2, D, FP, seed=int(cap))
+    check(ops, q, k, v, do, f"scale, cap {cap} bias {bias} {D}", cap=cap, slopes=slopes, scale=0.37)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_attention_masks(ops, dtype):
+    i32 = torch.int32
+    # prefixes: none, inside a tile, at a tile's end, beyond the keys, negative
+    q, k, v, do = inputs(5, 140, 140, 2, 1, 64, dtype)
+    check(ops, q, k, v, do, "prefix", causal=True, prefix=torch.tensor([0, 37, 128, 500, -4], dtype=i32))
+    # lengths: none, one key, inside a tile, all, beyond the slots (clamped), negative (clamped)
+    q, k, v, do = inputs(6, 70, 130, 2, 1, 64, dtype)
+    for causal in (False, True):
+        check(ops, q, k, v, do, f"lengths causal {causal}", causal=causal,
+              lengths=torch.tensor([0, 1, 67, 130, 999, -3], dtype=i32).clamp(0, 130))
+    # positions before the first key, across it, after the last key
+    q, k, v, do = inputs(4, 70, 130, 2, 1, 64, dtype)
+    check(ops, q, k, v, do, "starts", causal=True, starts=torch.tensor([-200, -30, 64, 300], dtype=i32),
+          slopes=torch.tensor([0.3, 0.02]))
+    # documents: packed, of one token, in any order, positions outside the keys
+    docs = torch.zeros(4, 200, dtype=i32)
+    docs[0, 64:] = 1
+    docs[1] = torch.arange(200) // 7
+    docs[2] = torch.arange(200)
+    docs[3] = torch.randint(0, 3, (200,), generator=torch.Generator().manual_seed(3)).to(i32) - 1
+    q, k, v, do = inputs(4, 200, 200, 4, 2, 64, dtype)
+    for causal in (False, True):
+        check(ops, q, k, v, do, f"documents causal {causal}", causal=causal, docs=docs)
+    q, k, v, do = inputs(4, 90, 200, 4, 2, 64, dtype)
+    check(ops, q, k, v, do, "documents, positions outside", docs=docs, starts=torch.tensor([-20, 150, 0, 250], dtype=i32))
+    check(ops, q, k, v, do, "all masks", causal=True, docs=docs, prefix=torch.tensor([10, 100, 3, 0], dtype=i32),
+          lengths=torch.tensor([180, 101, 200, 64], dtype=i32), starts=torch.tensor([100, 90, 110, 0], dtype=i32), cap=8.0,
+          slopes=torch.tensor([0.1, 0.2, 0.0, 1.0]))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_long_documents(ops, dtype, D):
+    """Many tiles, most of them skipped."""
+    S = 1500
+    docs = (torch.arange(S)[None] // 190).to(torch.int32)
+    q, k, v, do = inputs(1, S, S, 2, 1, D, dtype)
+    check(ops, q, k, v, do, f"long documents {D}", causal=True, docs=docs, cap=30.0)
+
+
+@pytest.mark.parametrize("dtype,D,group", [(BF, 64, 1), (FP, 64, 4), (BF, 128, 8), (FP, 80, 6), (BF, 96, 3)])
+def test_attention_few_tokens(ops, dtype, D, group):
+    """New tokens over caches: one to nine queries, keys split over workgroups and joined."""
+    for i, (B, Sq, Sk) in enumerate(((1, 1, 1), (2, 1, 63), (1, 1, 700), (3, 1, 2049), (2, 5, 3000), (1, 9, 5003), (5, 2, 517))):
+        q, k, v, do = inputs(B, Sq, Sk, 2 * group, 2, D, dtype, "heads" if i % 2 else "separate", seed=i)
+        lengths = torch.tensor([max(Sq, Sk - 37 * b * (Sk // 150)) for b in range(B)], dtype=torch.int32)
+        if B > 2:
+            lengths[1] = 0
+        check(ops, q, k, v, do, f"few tokens {B} {Sq} {Sk} {D}", causal=True, lengths=lengths, starts=lengths - Sq,
+              cap=15.0 if i % 3 == 0 else 0.0, slopes=torch.rand(2 * group) if i % 2 else None, backward=False)
+    q, k, v, do = inputs(2, 100, 2500, group, 1, D, dtype)
+    check(ops, q, k, v, do, f"split with more rows {D}", causal=False, backward=False)
+
+
+def test_attention_nothing_beyond_the_length(ops):
+    """NaN and infinities in the padding of a cache."""
+    q, k, v, do = inputs(2, 30, 300, 2, 1, 64, BF)
+    lengths = torch.tensor([77, 0], dtype=torch.int32)
+    for b in range(2):
+        k.data[b, int(lengths[b]):] = float("nan")
+        v.data[b, int(lengths[b]):] = float("inf")
+    check(ops, q, k, v, do, "padding", lengths=lengths)
+    check(ops, q, k, v, do, "padding, split", lengths=lengths, backward=False)
+
+
+def test_attention_empty(ops):
+    dev = "cuda"
+    for B, Sq, Sk in ((0, 4, 4), (2, 0, 5), (2, 5, 0), (1, 0, 0)):
+        q = torch.randn(B, Sq, 4, 64, device=dev, dtype=BF, requires_grad=True)
+        k, v = (torch.randn(B, Sk, 2, 64, device=dev, dtype=BF, requires_grad=True) for _ in range(2))
+        out, lse = ops.attention(q, k, v, return_lse=True)
+        assert out.shape == q.shape and not out.any()
+        assert (lse == -math.inf).all()
+        for t, g in zip((q, k, v), torch.autograd.grad(out, (q, k, v), torch.ones_like(out))):
+            assert g.shape == t.shape and not g.any()
+
+
+def test_attention_shared_inputs(ops):
+    """Gradients of keys that are broadcast over the batch and of one tensor used three times."""
+    q, k, v, do = inputs(3, 50, 50, 4, 2, 64, BF)
+    k1, v1 = k.detach()[:1].requires_grad_(), v.detach()[:1].requires_grad_()
+    ke, ve = k1.expand(3, -1, -1, -1), v1.expand(3, -1, -1, -1)
+    want, tol = definition(q, ke, ve, do, 0.125, 0.0, None, True, None, None, None, None)
+    out = ops.attention(q, ke, ve, causal=True)
+    dk, dv = torch.autograd.grad(out, (k1, v1), do)
+    # the sum over the batch is torch's, in bf16: at most a rounding of each partial sum
+    for n, g in (("dk", dk), ("dv", dv)):
+        close(g, want[n].sum(0, keepdim=True), tol[n].sum(0, keepdim=True) + 3 * U[BF] * want[n].abs().sum(0, keepdim=True), n)
+    x = torch.randn(2, 33, 3, 64, device="cuda", dtype=BF, requires_grad=True)
+    out = ops.attention(x, x, x)
+    g, = torch.autograd.grad(out, x, torch.ones_like(out))
+    want, tol = definition(x, x, x, torch.ones_like(out), 0.125, 0.0, None, False, None, None, None, None)
+    total = want["dq"] + want["dk"] + want["dv"]
+    size = want["dq"].abs() + want["dk"].abs() + want["dv"].abs()
+    close(g, total, tol["dq"] + tol["dk"] + tol["dv"] + 3 * U[BF] * size, "one tensor")
+
+
+def test_attention_differences(ops):
+    """The gradient against central differences of the forward pass, along
+    random directions.  In fp16 with n queries the forward's rounding, u |out|,
+    limits a difference: it is summed over the outputs as independent errors
+    (six standard deviations), and the third derivative's term is h^2."""
+    g = torch.Generator().manual_seed(5)
+    B, S, H, D = 1, 40, 2, 64
+    base = [torch.randn(B, S, H, D, generator=g).half() for _ in range(3)]
+    w = torch.randn(B, S, H, D, generator=g)
+    kw = dict(cap=4.0, slopes=torch.tensor([0.2, 0.05]).cuda(), causal=True, scale=0.125)
+    leaves = [t.cuda().requires_grad_() for t in base]
+    out = ops.attention(*leaves, **kw)
+    grads = torch.autograd.grad(out, leaves, w.half().cuda())
+    w16 = w.half().double()
+    h = 2.0 ** -4
+    for i in range(3):
+        d = torch.sign(torch.randn(B, S, H, D, generator=g))
+
+        def at(step):
+            x = [t.clone() for t in base]
+            x[i] = (x[i].double() + step * d).half()
+            o = ops.attention(*[t.cuda() for t in x], **kw).double().cpu()
+            return (o * w16).sum().item(), o, x[i].double()
+
+        fp, op, xp = at(h)
+        fm, om, xm = at(-h)
+        exact_step = (xp - xm)                            # what the rounded inputs really moved by
+        slope = (fp - fm)
+        want = (grads[i].double().cpu() * exact_step).sum().item()
+        noise = 6 * U[FP] * math.sqrt(((op.abs() * w16) ** 2).sum().item() * 2) + \
+            6 * U[FP] * 2 * math.sqrt(((grads[i].double().cpu() * exact_step) ** 2).sum().item())
+        curve = 4 * h * h * (grads[i].double().cpu().abs() * exact_step.abs()).sum().item()
+        assert abs(slope - want) <= noise + curve, (i, slope, want, noise, curve)
+
+
+def test_attention_same_bits(ops):
+    """A replay gives the same bits, on another stream and within a graph too."""
+    q, k, v, do = inputs(2, 300, 300, 4, 2, 128, BF)
+    kw = dict(causal=True, cap=20.0, docs=(torch.arange(300)[None] // 110).expand(2, -1).to(torch.int32).cuda())
+
+    def once():
+        out = ops.attention(q, k, v, **kw)
+        return (out.detach(), *torch.autograd.grad(out, (q, k, v), do))
+
+    first = once()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = once()
+    side.synchronize()
+    for a, b in zip(first, second):
+        assert torch.equal(a, b)
+    qs, ks, vs = q.detach()[:, :3].contiguous(), k.detach(), v.detach()
+    eager = ops.attention(qs, ks, vs, causal=True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = ops.attention(qs, ks, vs, causal=True)
+    for i in range(3):
+        qs.mul_(1.5)
+        want = ops.attention(qs, ks, vs, causal=True)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, want), i
+    assert eager.shape == held.shape
+
+
+# ---- dropout --------------------------------------------------------------------------
+
+def kept(n, p, seed, offset):
+    with np.errstate(over="ignore"):
+        def mix(z):
+            z = (z ^ (z >> np.uint64(30))) * np.uint64(0xBF58476D1CE4E5B9)
+            z = (z ^ (z >> np.uint64(27))) * np.uint64(0x94D049BB133111EB)
+            return z ^ (z >> np.uint64(31))
+
+        G = np.uint64(0x9E3779B97F4A7C15)
+        key = mix(np.array([seed % 2 ** 64], np.uint64) + G)
+        z = mix(key + G * (np.arange((n + 1) // 2, dtype=np.uint64) + np.uint64(offset % 2 ** 64)))
+        u = z.astype("<u8").view("<u4")[:n]
+    return torch.from_numpy(u.astype(np.int64) >= math.floor(p * 2.0 ** 32))
+
+
+SHAPES = [(1,), (7,), (8,), (2, 3), (1, 2049), (5, 16), (33, 1000), (3, 7, 40), (257, 255), (4, 1)]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP, F32])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 0.97, 1.0])
+def test_dropout(ops, dtype, p):
+    for i, shape in enumerate(SHAPES):
+        seed, offset = (-1, 2 ** 64 - 3, 12345678901234567)[i % 3], (0, 5, 2 ** 63 + 11)[i % 3]
+        g = torch.Generator().manual_seed(i)
+        x, r, do = (torch.randn(shape, generator=g).to(dtype).cuda() for _ in range(3))
+        n = x.numel()
+        keep = kept(n, p, seed, offset).view(shape)
+        x.requires_grad_()
+        inv = 1 / (1 - p) if p < 1 else 0.0
+        for res in (None, r):
+            out = ops.dropout_add(x, res, p=p, seed=seed, offset=offset)
+            want = x.detach().double().cpu() * keep * inv
+            size = want.abs()
+            if res is not None:
+                want, size = want + r.double().cpu(), size + r.double().cpu().abs()
+            close(out, want, U[dtype] * want.abs() + 2.0 ** -22 * size + TINY[dtype], f"dropout {shape} {p}")
+            dx, = torch.autograd.grad(out, x, do)
+            want = do.double().cpu() * keep * inv
+            close(dx, want, U[dtype] * want.abs() + 2.0 ** -22 * want.abs() + TINY[dtype], f"dx {shape} {p}")
+            assert torch.equal((dx != 0).cpu(), keep & (do.cpu() != 0))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_dropout_strides(ops, dtype):
+    """The mask goes by the element's number, not by the strides."""
+    base = torch.randn(40, 64, device="cuda", dtype=dtype)
+    keep = kept(40 * 64, 0.3, 9, 4).view(40, 64).cuda()
+    views = {"plain": base, "rows apart": torch.randn(40, 80, device="cuda", dtype=dtype)[:, 8:72],
+             "odd rows": torch.randn(40, 67, device="cuda", dtype=dtype)[:, 3:],
+             "transposed": torch.randn(64, 40, device="cuda", dtype=dtype).t(),
+             "broadcast": torch.randn(1, 64, device="cuda", dtype=dtype).expand(40, 64),
+             "backwards in pairs": torch.randn(20, 2, 64, device="cuda", dtype=dtype).transpose(0, 1).reshape(40, 64)}
+    for name, x in views.items():
+        for rname, r in views.items():
+            out = ops.dropout_add(x, r, p=0.3, seed=9, offset=4)
+            part = torch.where(keep, x.double() / 0.7, 0.0)
+            want = part + r.double()
+            close(out, want.cpu(), (U[dtype] * want.abs() + 2.0 ** -22 * (part.abs() + r.double().abs())).cpu(), name + rname)
+    three = torch.randn(5, 8, 96, device="cuda", dtype=dtype)[:, :, :64]
+    out = ops.dropout_add(three, p=0.3, seed=9, offset=4)
+    assert torch.equal(out != 0, keep.view(5, 8, 64) & (three != 0))
+
+
+def test_dropout_drops_anything(ops):
+    """Dropped infinities and NaN leave nothing; kept ones stay; residuals pass."""
+    n = 4096
+    keep = kept(n, 0.5, 1, 0).cuda()
+    x = torch.full((n,), float("nan"), device="cuda", dtype=BF)
+    x[::2] = float("inf")
+    out = ops.dropout_add(x, p=0.5, seed=1)
+    assert (out[~keep] == 0).all() and not torch.isfinite(out[keep]).any()
+    assert (ops.dropout_add(x, p=1.0, seed=1) == 0).all()
+    r = torch.randn(n, device="cuda", dtype=BF, requires_grad=True)
+    out = ops.dropout_add(torch.zeros_like(r), r, p=0.5, seed=1)
+    assert torch.equal(out, r)
+    assert torch.equal(torch.autograd.grad(out, r, torch.ones_like(r))[0], torch.ones_like(r))
+    assert ops.dropout_add(torch.empty(0, 5, device="cuda"), p=0.5, seed=1).shape == (0, 5)
+
+
+def test_dropout_parts_make_the_whole(ops):
+    """Calls whose offsets follow one another draw what one call draws."""
+    x = torch.randn(1000, 64, device="cuda", dtype=BF)
+    whole = ops.dropout_add(x, p=0.2, seed=77, offset=100)
+    first, rest = ops.dropout_add(x[:300], p=0.2, seed=77, offset=100), ops.dropout_add(x[300:], p=0.2, seed=77,
+                                                                                     offset=100 + 300 * 32)
+    assert torch.equal(whole, torch.cat([first, rest]))
+    share = (whole == 0).double().mean().item()          # 64000 draws: six standard deviations are 0.0095
+    assert abs(share - 0.2) < 0.0095
+    assert not torch.equal(whole == 0, ops.dropout_add(x, p=0.2, seed=78, offset=100) == 0)
+
+
+# ---- log probabilities ----------------------------------------------------------------------
+
+def logprobs_definition(x, tok, top, dlogp, dent, dtop):
+    u, tiny = U[x.dtype], TINY[x.dtype]
+    x, tok = x.detach().double().cpu(), tok.cpu()
+    T, V = x.shape
+    L = torch.logsumexp(x, 1)
+    nothing = L == -math.inf
+    logq = torch.where(nothing[:, None], -math.inf, x - L[:, None])
+    q = torch.exp(logq)
+    fin = torch.where(q > 0, logq, 0.0)
+    H = -(q * fin).sum(1)
+    has, over = tok >= 0, tok >= V
+    at = torch.gather(logq, 1, tok.clamp(0, V - 1)[:, None])[:, 0]
+    logp = torch.where(has, at, 0.0)
+    # 32-bit sums: a lane adds up to V / 64 terms, six joins; exp2 of an argument rounded to 2^-24 of itself
+    rel = 2.0 ** -24 * (V / 64 + 40 + 4 * (q * fin.abs()).sum(1))
+    mag = x.masked_fill(torch.isinf(x), 0).abs().amax(1) + L.abs().nan_to_num(0, 0, 0)
+    tol = dict(logp=rel + 2.0 ** -22 * mag, entropy=rel * (1 + H.abs() * 2) + 2.0 ** -22 * (1 + H.abs()) + 2.0 ** -21 * mag)
+    res = dict(logp=logp, entropy=torch.where(nothing, 0.0, H))
+    G = torch.where(has, dlogp.double().cpu(), 0.0) if dlogp is not None else torch.zeros(T, dtype=torch.float64)
+    dx = torch.zeros_like(x)
+    dx.scatter_add_(1, tok.clamp(0, V - 1)[:, None], torch.where(over, 0.0, G)[:, None])
+    total = G.clone()
+    size = G.abs()
+    if top:
+        order = torch.sort(x, dim=1, descending=True, stable=True)[1][:, :top]
+        res["top_ids"] = order
+        res["top_logp"] = torch.gather(logq, 1, order)
+        tol["top_logp"] = tol["logp"][:, None].expand(T, top)
+        if dtop is not None:
+            dx.scatter_add_(1, order, dtop.double().cpu())
+            total = total + dtop.double().cpu().sum(1)
+            size = size + dtop.double().cpu().abs().sum(1)
+    dh = dent.double().cpu() if dent is not None else torch.zeros(T, dtype=torch.float64)
+    inner = total[:, None] + dh[:, None] * (fin + H[:, None])
+    dx = dx - q * inner
+    dx[nothing] = 0
+    e = (rel + 2.0 ** -22 * mag)[:, None] * 4 + 2.0 ** -22 * fin.abs()
+    tol["dx"] = u * dx.abs() + q * (e * (size[:, None] + dh.abs()[:, None] * (1 + fin.abs() + H[:, None].abs()))) + \
+        2.0 ** -21 * size[:, None] * (dx != 0) * q.clamp_min(2.0 ** -30) + 2.0 ** -22 * dx.abs() + tiny
+    res["dx"] = dx
+    return res, tol
+
+
+def check_logprobs(ops, x, tok, top, label, dtop_too=True):
+    print(label, flush=True)
+    T, V = x.shape
+    g = torch.Generator().manual_seed(T + V)
+    dlogp, dent = torch.randn(T, generator=g).cuda(), torch.randn(T, generator=g).cuda()
+    dtop = torch.randn(T, top, generator=g).cuda() if top else None
+    want, tol = logprobs_definition(x, tok, top, dlogp, dent, dtop)
+    with torch.no_grad():
+        plain = ops.token_logprobs(x, tok, top=top)
+    x = x.detach().requires_grad_()
+    r = ops.token_logprobs(x, tok, top=top)
+    assert torch.equal(r.logp, plain.logp) and torch.equal(r.entropy, plain.entropy)
+    close(r.logp, want["logp"], tol["logp"], label + " logp")
+    close(r.entropy, want["entropy"], tol["entropy"], label + " entropy")
+    outs, grads = [r.logp, r.entropy], [dlogp, dent]
+    if top:
+        assert torch.equal(r.top_ids.cpu(), want["top_ids"]), label
+        close(r.top_logp, want["top_logp"], tol["top_logp"], label + " top")
+        outs.append(r.top_logp)
+        grads.append(dtop)
+    dx, = torch.autograd.grad(outs, x, grads)
+    close(dx, want["dx"], tol["dx"], label + " dx")
+
+
+VOCABS = [1, 2, 7, 8, 9, 63, 64, 65, 255, 512, 513, 2047, 2048, 2051, 4100, 8191, 8192, 8203, 30011]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP, F32])
+def test_logprobs_sizes(ops, dtype):
+    for V in VOCABS:
+        for T in ((1, 5) if V > 600 else (1, 9)):
+            g = torch.Generator().manual_seed(V * 10 + T)
+            x = (torch.randn(T, V, generator=g) * 3).to(dtype).cuda()
+            tok = torch.randint(0, V, (T,), generator=g).cuda()
+            tok[T // 2] = -100 if T > 1 else 0
+            check_logprobs(ops, x, tok, min(V, 0 if V % 2 else 5), f"{dtype} T {T} V {V}")
+
+
+@pytest.mark.parametrize("top", [1, 2, 20, 32])
+@pytest.mark.parametrize("order", ["random", "rising", "falling", "equal", "two values"])
+def test_logprobs_alternatives(ops, top, order):
+    """Orders that make every element a candidate, and ties."""
+    for T, V in ((3, 300), (2, 5000), (300, 9001), (1, 70001)):
+        if order == "random":
+            x = torch.randn(T, V, generator=torch.Generator().manual_seed(V))
+        elif order == "equal":
+            x = torch.full((T, V), 0.5)
+        elif order == "two values":
+            x = torch.randint(0, 2, (T, V), generator=torch.Generator().manual_seed(V)).float()
+        else:
+            x = torch.arange(V).float().expand(T, V) * (2.0 ** -10) * (1 if order == "rising" else -1)
+        tok = torch.arange(T) % V
+        x = x.contiguous().to(F32 if V != 9001 else BF).cuda()
+        with torch.no_grad():
+            r = ops.token_logprobs(x, tok.cuda(), top=top)
+        want = torch.sort(x.cpu(), dim=1, descending=True, stable=True)[1][:, :top]
+        assert torch.equal(r.top_ids.cpu(), want), (T, V)
+
+
+def test_logprobs_masked_vocabulary(ops):
+    for dtype in (BF, F32):
+        for T, V in ((6, 100), (6, 5000), (3, 20011)):
+            x = torch.randn(T, V, generator=torch.Generator().manual_seed(1)).to(dtype)
+            x[0] = -math.inf                              # nothing left
+            x[1, 3:] = -math.inf                          # fewer than the alternatives
+            x[2, ::2] = -math.inf
+            if T > 3:
+                x[3] = torch.finfo(dtype).min             # the type's lowest value everywhere
+                x[4, 1:] = torch.finfo(dtype).min
+                x[5] = 88.0
+            tok = torch.tensor([5, 1, 3, 7, 0, -1][:T])
+            check_logprobs(ops, x.cuda(), tok.cuda(), 6, f"masked {dtype} {V}")
+
+
+def test_logprobs_not_numbers(ops):
+    for T, V in ((4, 90), (4, 6001)):
+        x = torch.randn(T, V).cuda()
+        x[0, 3] = math.nan
+        x[1, V - 1] = math.inf
+        x[2] = math.nan
+        tok = torch.tensor([1, 2, 3, V], device="cuda")
+        r = ops.token_logprobs(x.requires_grad_(), tok, top=4)
+        for n in (r.logp, r.entropy, r.top_logp[:, 0]):
+            assert torch.isnan(n[:3]).all()
+        assert torch.isnan(r.logp[3]) and torch.isfinite(r.entropy[3])
+        assert ((r.top_ids >= 0) & (r.top_ids < V)).all()
+        dx, = torch.autograd.grad(r.logp.sum(), x)
+        assert torch.isnan(dx).any(1).all()
+
+
+def test_logprobs_strides(ops):
+    wide = torch.randn(6, 7000, device="cuda", dtype=BF)
+    tok = torch.tensor([0, 5, 6, -1, 9, 3000], device="cuda")
+    check_logprobs(ops, wide[:, 5:5006], tok, 3, "columns of a wider table")
+    check_logprobs(ops, wide[::2, :4096], tok[::2], 3, "every other row")
+    check_logprobs(ops, wide[:1].expand(6, 7000), tok, 2, "one row for all")
+    check_logprobs(ops, torch.randn(5000, 6, device="cuda").t(), tok, 2, "transposed")
+    x = torch.randn(2, 3, 5001, device="cuda")
+    r = ops.token_logprobs(x, tok.view(2, 3), top=2)
+    assert r.logp.shape == (2, 3) and r.top_ids.shape == (2, 3, 2)
+    flat = ops.token_logprobs(x.view(6, 5001), tok, top=2)
+    assert torch.equal(flat.logp, r.logp.view(-1)) and torch.equal(flat.top_ids, r.top_ids.view(6, 2))
+    empty = ops.token_logprobs(x[:0], tok.view(2, 3)[:0])
+    assert empty.logp.shape == (0, 3)
+
+
+def test_logprobs_one_gradient_at_a_time(ops):
+    x = torch.randn(5, 3000, device="cuda", requires_grad=True)
+    tok = torch.arange(5, device="cuda")
+    r = ops.token_logprobs(x, tok, top=2)
+    z = torch.log_softmax(x.double(), 1)
+    for got, want in ((r.logp.sum(), z[torch.arange(5), tok].sum()), (r.entropy.sum(), -(z.exp() * z).sum()),
+                      (r.top_logp.sum(), z.topk(2, dim=1)[0].sum())):
+        a, = torch.autograd.grad(got, x, retain_graph=True)
+        b, = torch.autograd.grad(want, x, retain_graph=True)
+        assert (a.double() - b.double()).abs().max() < 2.0 ** -18
+
+
+def test_logprobs_differences(ops):
+    """Against central differences in 64 bits of the definition, along a direction, and of the operator itself."""
+    g = torch.Generator().manual_seed(2)
+    x = torch.randn(4, 2500, generator=g).cuda().requires_grad_()
+    d = torch.randn(4, 2500, generator=g).cuda()
+    tok = torch.tensor([3, 4, 5, -1], device="cuda")
+    w = torch.tensor([1.0, -2.0, 0.5, 3.0], device="cuda")
+    r = ops.token_logprobs(x, tok)
+    dx, = torch.autograd.grad((r.logp, r.entropy), x, (w, 0.3 * w))
+    h = 2.0 ** -6
+    with torch.no_grad():
+        ends = []
+        for s in (h, -h):
+            y = ops.token_logprobs(x + s * d, tok)
+            ends.append((y.logp.double() * w).sum() + 0.3 * (y.entropy.double() * w).sum())
+    slope = ((ends[0] - ends[1]) / (2 * h)).item()
+    # 32-bit results of magnitude 10 differ by 2^-21 at most, divided by 2 h; the cubic term is of the order h^2
+    assert abs(slope - (dx.double() * d.double()).sum().item()) < 8 * 10 * 2.0 ** -21 / (2 * h) * 6.5 + 8 * h * h
+
+
+def test_logprobs_graph(ops):
+    x = torch.randn(2, 60000, device="cuda", dtype=BF)
+    tok = torch.tensor([1, 2], device="cuda")
+    ops.token_logprobs(x, tok, top=5)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = ops.token_logprobs(x, tok, top=5)
+    for _ in range(3):
+        x.copy_(torch.randn_like(x))
+        want = ops.token_logprobs(x, tok, top=5)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b)
+
+
+# ---- refusals ------------------------------------------------------------------------------
+
+def test_refusals(ops):
+    q = torch.randn(2, 5, 4, 64, device="cuda", dtype=BF)
+    k = torch.randn(2, 7, 2, 64, device="cuda", dtype=BF)
+    n = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for bad in (lambda: ops.attention(q[0], k, k), lambda: ops.attention(q, k, k[:, :6]),
+                lambda: ops.attention(q, k[..., :56], k[..., :56]), lambda: ops.attention(q, k, k, lengths=n[:1]),
+                lambda: ops.attention(q, k, k, docs=torch.zeros(2, 5, dtype=torch.int32, device="cuda")),
+                lambda: ops.attention(q, k, k, starts=n.cpu()), lambda: ops.attention(q, k, k, slopes=torch.zeros(3).cuda()),
+                lambda: ops.attention(q.cpu(), k.cpu(), k.cpu()),
+                lambda: ops.dropout_add(q, q[:1], p=0.1, seed=0), lambda: ops.dropout_add(q, p=1.5, seed=0),
+                lambda: ops.dropout_add(q, p=float("nan"), seed=0), lambda: ops.dropout_add(q.cpu(), p=0.1, seed=0),
+                lambda: ops.token_logprobs(q, n), lambda: ops.token_logprobs(q[0, 0], n.new_zeros(4).long(), top=65),
+                lambda: ops.token_logprobs(q[:, :, 0, :0], n.new_zeros(2, 5).long())):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: ops.attention(q.float(), k.float(), k.float()), lambda: ops.attention(q, k.half(), k.half()),
+                lambda: ops.attention(q, k, k, lengths=n.float()), lambda: ops.dropout_add(q.double(), p=0.1, seed=0),
+                lambda: ops.token_logprobs(q[0, 0], torch.zeros(4, device="cuda"))):
+        with pytest.raises(TypeError):
+            bad()
+    from paper_2006_09616_amd.dtr import DtrError
+    for bad, why in ((lambda: ops.attention(q[:, :, :3], k, k), "multiple of 2 key heads"),
+                     (lambda: ops.attention(q[..., :60], k[..., :60], k[..., :60]), "multiple of 8"),
+                     (lambda: ops.attention(q, k, k, prefix=n), "causal"), (lambda: ops.attention(q, k, k, cap=-1.0), "cap"),
+                     (lambda: ops.attention(q, k, k, scale=0.0), "scale"),
+                     (lambda: ops.attention(q, k, k, scale=float("inf")), "scale")):
+        with pytest.raises(DtrError) as e:
+            bad()
+        assert why in str(e.value)
