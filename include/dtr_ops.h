@@ -70,8 +70,8 @@ typedef struct {
 } dtr_attn;
 
 /* A tensor [batch][position][head][head_dim]: strides in elements, the last
- * dimension contiguous; data 16-byte aligned and strides multiples of 8.
- * Input strides may be 0 (broadcast). */
+ * dimension contiguous; data 16-byte aligned and strides multiples of 8,
+ * that of positions below 2^26.  Input strides may be 0 (broadcast). */
 typedef struct {
     void *data;
     int64_t batch, position, head;
@@ -79,13 +79,18 @@ typedef struct {
 
 int dtr_attn_workspace_bytes(const dtr_attn *attn, int32_t backward, size_t *bytes);
 
-/* out like q; lse [batch][q_heads][q_len] 32-bit, NULL if no backward follows. */
+/* out like q; lse [batch][q_heads][q_len] 32-bit, NULL if no backward follows.
+ * rest [batch][q_len][q_heads][head_dim] (contiguous, the inputs' type; or
+ * NULL) receives what the rounding took from out.  With it the backward pass
+ * knows out . dout, which it subtracts from every score gradient of a row, to
+ * twice the digits; without it dq and dk lose about a third of a bit. */
 int dtr_attn_forward(const dtr_attn *attn, const dtr_heads *q, const dtr_heads *k, const dtr_heads *v,
-                     const dtr_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+                     const dtr_heads *out, void *rest, float *lse, void *workspace, size_t workspace_bytes,
+                     void *stream);
 
-/* Gradients dq, dk, dv of the forward pass that gave out and lse. */
+/* Gradients dq, dk, dv of the forward pass that gave out, rest (or NULL) and lse. */
 int dtr_attn_backward(const dtr_attn *attn, const dtr_heads *q, const dtr_heads *k, const dtr_heads *v,
-                      const dtr_heads *out, const float *lse, const dtr_heads *dout,
+                      const dtr_heads *out, const void *rest, const float *lse, const dtr_heads *dout,
                       const dtr_heads *dq, const dtr_heads *dk, const dtr_heads *dv,
                       void *workspace, size_t workspace_bytes, void *stream);
 

@@ -31,7 +31,7 @@ struct Bf16 {
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
-    static constexpr float p_gain = 1.0f;
+    static constexpr float p_gain = 1.0f, p_shift = 0.0f;
 };
 // Backward probabilities of long rows are below the smallest normal number
 // of fp16; 2^6 keeps six more bits of them (they are at most 1).
@@ -42,7 +42,7 @@ struct Fp16 {
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
-    static constexpr float p_gain = 64.0f;
+    static constexpr float p_gain = 64.0f, p_shift = 6.0f;
 };
 
 // eight numbers rounded to the inputs' type: an operand of the next product
@@ -95,29 +95,40 @@ template <int NB> struct Tile {
     }
 };
 
-// ROWS rows of a tensor on their way to LDS, 256 threads; rows from `end` on
-// and columns from head_dim on are zero.
-template <int NB, int ROWS> struct Staged {
+// 64 rows of a tensor (consecutive positions of a head) on their way to LDS,
+// 256 threads; rows from `end` on and columns from head_dim on are zero.  The
+// address is a uniform base and a 32-bit offset of the lane.
+constexpr int STAGE_ROWS = 64;
+
+template <int NB> struct Staged {
     using L = Tile<NB>;
-    static constexpr int N = ROWS * L::CHUNKS / 256;
+    static constexpr int N = STAGE_ROWS * L::CHUNKS / 256, STEP = 256 / L::CHUNKS;
     uint4 r[N];
     __device__ void load(const char *base, int64_t stride, int row0, int end, int head_dim)
     {
-        const int c = threadIdx.x % L::CHUNKS;
+        const int c = threadIdx.x % L::CHUNKS, i = threadIdx.x / L::CHUNKS;
+        const char *p = base + row0 * stride * 2;
+        const uint32_t off = (uint32_t)(i * (uint32_t)stride + c * 8) * 2u;
 #pragma unroll
-        for (int n = 0; n < N; n++) {
-            const int row = row0 + threadIdx.x / L::CHUNKS + n * (256 / L::CHUNKS);
-            r[n] = row < end && c * 8 < head_dim ? *(const uint4 *)(base + ((int64_t)row * stride + c * 8) * 2)
-                                                 : make_uint4(0, 0, 0, 0);
+        for (int n = 0; n < N; n++) r[n] = make_uint4(0, 0, 0, 0);
+        if (c * 8 >= head_dim) return;
+        if (row0 + STAGE_ROWS <= end) {
+#pragma unroll
+            for (int n = 0; n < N; n++) r[n] = *(const uint4 *)(p + n * STEP * stride * 2 + off);
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; n++)
+                if (row0 + i + n * STEP < end) r[n] = *(const uint4 *)(p + n * STEP * stride * 2 + off);
         }
     }
     __device__ void store(short *tile) const
     {
-        const int c = threadIdx.x % L::CHUNKS;
+        const int c = threadIdx.x % L::CHUNKS, i = threadIdx.x / L::CHUNKS;
 #pragma unroll
-        for (int n = 0; n < N; n++) *(uint4 *)(tile + L::at(threadIdx.x / L::CHUNKS + n * (256 / L::CHUNKS), c)) = r[n];
+        for (int n = 0; n < N; n++) *(uint4 *)(tile + L::at(i + n * STEP, c)) = r[n];
     }
 };
+static_assert(STAGE_ROWS == KEY_TILE, "a tile of keys is staged at once");
 
 // Rows of one key head in packed order: row = query * group + head of the
 // group, so that a tile holds the group's heads of few queries and reads the
@@ -169,39 +180,63 @@ __global__ void __launch_bounds__(64) doc_tiles_kernel(AttnArgs a)
     }
 }
 
-// ---- forward -----------------------------------------------------------------
-// A workgroup has 128 rows, a wavefront 32, and walks over tiles of 64 keys.
+template <typename R> struct Four { typedef R v __attribute__((ext_vector_type(4))); };
 
-template <typename T, int NB, bool CAP>
-__global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
+template <typename T>
+__device__ __forceinline__ void write_four(const Heads &t, int b, int head, int64_t position, int col, f32x4 v)
 {
-    using L = Tile<NB>;
     using R = typename T::raw;
-    __shared__ __align__(16) short ks[KEY_TILE * L::PITCH], vs[KEY_TILE * L::PITCH];
-    __shared__ int range[4];                            // first and last active tile, least and greatest document
+    typename Four<R>::v r;
+#pragma unroll
+    for (int i = 0; i < 4; i++) r[i] = (R)v[i];
+    *(typename Four<R>::v *)(t.data + (b * t.batch + head * t.head + position * t.position + col) * 2) = r;
+}
 
-    const int row_tiles = (a.rows + ROW_TILE - 1) / ROW_TILE;
-    const int units = a.batch * a.k_heads;
-    int id = spread(blockIdx.x, gridDim.x);
-    const int split = id % a.splits;
-    id /= a.splits;
-    const Unit u(a, id / row_tiles);
-    const int tile_row = (row_tiles - 1 - id % row_tiles) * ROW_TILE;      // the longest first under a causal mask
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, hi = lane / 32;
+// Four columns of the output and, for the backward pass, what the rounding
+// took from them: out . dout is subtracted from every score gradient of its
+// row, so that its error does not average out over the keys.
+template <typename T>
+__device__ __forceinline__ void write_out(const AttnArgs &a, int b, int head, int query, int col, f32x4 v)
+{
+    using R = typename T::raw;
+    write_four<T>(a.out, b, head, query, col, v);
+    if (a.rest) {
+        typename Four<R>::v r;
+#pragma unroll
+        for (int i = 0; i < 4; i++) r[i] = (R)(v[i] - (float)(R)v[i]);
+        *(typename Four<R>::v *)(a.rest + (((int64_t)b * a.q_len + query) * a.k_heads * a.group + head) * a.head_dim * 2 + col * 2) = r;
+    }
+}
 
-    const int row = tile_row + wave * 32 + lane % 32;
-    const int crow = min(row, a.rows - 1);
-    const int query = crow / a.group, head = u.g * a.group + crow % a.group;
-    const int pos = u.start + query;
-    const int p_first = u.start + tile_row / a.group, p_last = u.start + min(tile_row + ROW_TILE - 1, a.rows - 1) / a.group;
-    const bool has_doc = !u.docs || (pos >= 0 && pos < a.k_len);
-    const int doc = u.docs && has_doc ? u.docs[pos] : 0;
-    const int row_end = has_doc ? u.end(a, pos) : 0;
+// The rows of a workgroup (32 a wavefront, one a lane pair) and the tiles of
+// keys that any of them may see.
+struct RowBlock {
+    Unit u;
+    int row, query, head, pos, doc, end;     // of the lane's row; keys from `end` on are masked for it
+    int sure;                                // keys before `sure` are seen by all rows, but for documents
+    int wave_end;                            // keys from here on are masked for all rows of the wavefront
+    int t0, t1;                              // tiles
+    int doc_lo, doc_hi;
+    bool one_doc;
 
-    // tiles that any row of the workgroup may see
-    int t0 = 0, t1 = (u.end(a, p_last) + KEY_TILE - 1) / KEY_TILE, doc_lo = 0, doc_hi = 0;
-    bool one_doc = true;
-    if (u.docs) {
+    __device__ RowBlock(const AttnArgs &a, int unit, int tile_row, int (&range)[4]) : u(a, unit)
+    {
+        const int wave = threadIdx.x / WAVE, last = a.rows - 1;
+        row = tile_row + wave * 32 + threadIdx.x % 32;
+        const int r = min(row, last);
+        query = r / a.group;
+        head = u.g * a.group + r % a.group;
+        pos = u.start + query;
+        const bool has_doc = !u.docs || (pos >= 0 && pos < a.k_len);
+        doc = u.docs && has_doc ? u.docs[pos] : 0;
+        end = has_doc ? u.end(a, pos) : 0;
+        sure = u.end(a, u.start + tile_row / a.group);
+        wave_end = u.end(a, u.start + min(tile_row + wave * 32 + 31, last) / a.group);
+        t0 = 0;
+        t1 = (u.end(a, u.start + min(tile_row + ROW_TILE - 1, last) / a.group) + KEY_TILE - 1) / KEY_TILE;
+        doc_lo = doc_hi = 0;
+        one_doc = true;
+        if (!u.docs) return;
         if (threadIdx.x == 0) {
             range[0] = INT32_MAX;
             range[1] = -1;
@@ -214,112 +249,181 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
             atomicMax(&range[3], doc);
         }
         one_doc = __syncthreads_and(has_doc);
-        doc_lo = range[2];
-        doc_hi = range[3];
-        for (int t = threadIdx.x; t < t1; t += 256) {
-            const int2 d = u.doc_tiles[t];
-            if (d.x <= doc_hi && d.y >= doc_lo) {
+        doc_lo = __builtin_amdgcn_readfirstlane(range[2]);
+        doc_hi = __builtin_amdgcn_readfirstlane(range[3]);
+        for (int t = threadIdx.x; t < t1; t += 256)
+            if (near(t)) {
                 atomicMin(&range[0], t);
                 atomicMax(&range[1], t);
             }
-        }
         __syncthreads();
-        t0 = range[0];
-        t1 = range[1] + 1;
+        t0 = __builtin_amdgcn_readfirstlane(range[0]);
+        t1 = __builtin_amdgcn_readfirstlane(range[1]) + 1;
         one_doc = one_doc && doc_lo == doc_hi;
     }
-    if (a.splits > 1) {                                  // this part's tiles
-        const int n = max(t1 - t0, 0), per = (n + a.splits - 1) / a.splits;
-        t0 = min(t0, t1) + per * split;
-        t1 = min(t0 + per, t1);
+    // whether a tile's documents and the rows' overlap
+    __device__ bool near(int t) const
+    {
+        const int2 d = u.doc_tiles[t];
+        return d.x <= doc_hi && d.y >= doc_lo;
     }
+    __device__ int next(int t) const
+    {
+        if (u.docs)
+            while (t < t1 && !near(t)) t++;
+        return t;
+    }
+    // whether every row sees every key of the tile
+    __device__ bool whole(int t) const
+    {
+        bool w = (t + 1) * KEY_TILE <= sure;
+        if (u.docs) {
+            const int2 d = u.doc_tiles[t];
+            w = w && one_doc && d.x == d.y;
+        }
+        return w;
+    }
+    __device__ bool sees(const AttnArgs &a, int key) const
+    {
+        return key < end && (!u.docs || u.docs[min(key, a.k_len - 1)] == doc);
+    }
+};
+
+// ---- forward -----------------------------------------------------------------
+// A workgroup has 128 rows, a wavefront 32, and walks over tiles of 64 keys.
+// The next tile is on its way from memory to registers while one is worked
+// on in LDS (two buffers, one barrier a tile).
+
+template <typename T, int NB, bool SHAPED>
+__global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
+{
+    using L = Tile<NB>;
+    using R = typename T::raw;
+    constexpr int SIZE = KEY_TILE * L::PITCH;
+    __shared__ __align__(16) short tiles[4 * SIZE];     // two of keys, two of values
+    __shared__ int range[4];
+
+    const int row_tiles = (a.rows + ROW_TILE - 1) / ROW_TILE;
+    const int units = a.batch * a.k_heads;
+    int id = spread(blockIdx.x, gridDim.x);
+    const int split = id % a.splits;
+    id /= a.splits;
+    // the longest first under a causal mask
+    RowBlock w(a, id / row_tiles, (row_tiles - 1 - id % row_tiles) * ROW_TILE, range);
+    if (a.splits > 1) {                                  // this part's tiles
+        const int n = max(w.t1 - w.t0, 0), per = (n + a.splits - 1) / a.splits;
+        w.t0 = min(w.t0, w.t1) + per * split;
+        w.t1 = min(w.t0 + per, w.t1);
+    }
+    const Unit &u = w.u;
+    const int lane = threadIdx.x % WAVE, hi = lane / 32;
 
     s16x8 q[2 * NB];
     {
-        const char *qp = head_base(a.q, u.b, head) + query * a.q.position * 2;
+        const char *qp = head_base(a.q, u.b, w.head) + w.query * a.q.position * 2;
 #pragma unroll
         for (int s = 0; s < 2 * NB; s++) {
             const int d = 16 * s + 8 * hi;
             q[s] = d < a.head_dim ? *(const s16x8 *)(qp + d * 2) : s16x8{};
         }
     }
-    const float slope2 = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
-    const float scale2 = CAP ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    const bool capped = a.cap > 0, bias = a.slopes != nullptr;
+    const float slope2 = bias ? a.slopes[w.head] * LOG2E : 0.0f;
+    const float scale2 = capped ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
 
     f32x16 o[NB] = {};
     float m = LOWEST, l = 0;
     const char *kb = head_base(a.k, u.b, u.g), *vb = head_base(a.v, u.b, u.g);
 
-    for (int t = t0; t < t1; t++) {
-        const int j0 = t * KEY_TILE;
-        bool in_doc = true;
-        if (u.docs) {
-            const int2 d = u.doc_tiles[t];
-            if (d.x > doc_hi || d.y < doc_lo) continue;
-            in_doc = one_doc && d.x == d.y;
+    int t = w.next(w.t0);
+    Staged<NB> sk, sv;
+    if (t < w.t1) {
+        sk.load(kb, a.k.position, t * KEY_TILE, u.len, a.head_dim);
+        sv.load(vb, a.v.position, t * KEY_TILE, u.len, a.head_dim);
+        sk.store(tiles);
+        sv.store(tiles + 2 * SIZE);
+    }
+    __syncthreads();
+    for (int buf = 0; t < w.t1; buf ^= 1) {
+        const int j0 = t * KEY_TILE, t2 = w.next(t + 1);
+        if (t2 < w.t1) {
+            sk.load(kb, a.k.position, t2 * KEY_TILE, u.len, a.head_dim);
+            sv.load(vb, a.v.position, t2 * KEY_TILE, u.len, a.head_dim);
         }
-        Staged<NB, KEY_TILE> sk, sv;
-        sk.load(kb, a.k.position, j0, u.len, a.head_dim);
-        sv.load(vb, a.v.position, j0, u.len, a.head_dim);
-        __syncthreads();
-        sk.store(ks);
-        sv.store(vs);
-        __syncthreads();
-        const bool whole = in_doc && j0 + KEY_TILE <= u.end(a, p_first);
-
-        f32x16 s[2] = {};
-#pragma unroll
-        for (int kbk = 0; kbk < 2; kbk++)
+        if (j0 < w.wave_end) {
+            const short *ks = tiles + buf * SIZE;
+            short *vs = tiles + (2 + buf) * SIZE;
+            f32x16 s[2] = {};
 #pragma unroll
             for (int st = 0; st < 2 * NB; st++)
-                s[kbk] = T::mfma(L::row_operand(ks, 32 * kbk + lane % 32, st), q[st], s[kbk]);
-
-        float x[32];
-        const float pf = (float)(pos - j0 - 4 * hi);
-        float most = LOWEST;
 #pragma unroll
-        for (int i = 0; i < 32; i++) {
-            const int c = 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4;          // key j0 + 4 hi + c
-            float v = s[i / 16][i % 16] * scale2;
-            if (CAP) v = cap2 * tanh_of(v);
-            if (a.slopes) v -= slope2 * fabsf(pf - (float)c);
-            x[i] = v;
-        }
-        if (!whole) {
+                for (int kb2 = 0; kb2 < 2; kb2++)
+                    s[kb2] = T::mfma(L::row_operand(ks, 32 * kb2 + lane % 32, st), q[st], s[kb2]);
+            // x: the scores times log2(e); plain ones but for a factor left to the exponent's fma
+            float x[32];
+            const float gain = SHAPED ? 1.0f : scale2;
+#pragma unroll
+            for (int i = 0; i < 32; i++) x[i] = s[i / 16][i % 16];
+            if (SHAPED) {
+                if (capped) {
+#pragma unroll
+                    for (int i = 0; i < 32; i++) x[i] = cap2 * tanh_of(x[i] * scale2);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; i++) x[i] *= scale2;
+                }
+                if (bias) {
+                    const float pf = (float)(w.pos - j0 - 4 * hi);
+#pragma unroll
+                    for (int i = 0; i < 32; i++) {
+                        const int c = 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4;      // key j0 + 4 hi + c
+                        x[i] -= slope2 * fabsf(pf - (float)c);
+                    }
+                }
+            }
+            if (!w.whole(t)) {
+#pragma unroll
+                for (int i = 0; i < 32; i++)
+                    x[i] = w.sees(a, j0 + 4 * hi + 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4) ? x[i] : -INFINITY;
+            }
+            float most = x[0];
+#pragma unroll
+            for (int i = 1; i < 32; i++) most = fmaxf(most, x[i]);
+            most = fmaxf(most, other_half(most)) * gain;
+            // The sums are moved to a new maximum only where the old one would let
+            // them grow by more than 2^8: 32-bit sums have room, and a probability
+            // is rounded relative to itself.
+            if (__any(most > m + 8.0f)) {
+                const float m_new = fmaxf(m, most), f = exp2_(m - m_new);
+                m = m_new;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < NB; d++) o[d] *= f;
+            }
 #pragma unroll
             for (int i = 0; i < 32; i++) {
-                const int j = j0 + 4 * hi + 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4;
-                bool seen = j < row_end;
-                if (u.docs) seen = seen && u.docs[min(j, a.k_len - 1)] == doc;
-                x[i] = seen ? x[i] : -INFINITY;
+                x[i] = exp2_(fmaf(x[i], gain, -m));
+                l += x[i];
+            }
+#pragma unroll
+            for (int kc = 0; kc < 4; kc++) {
+                const s16x8 p = rounded<T>(x + 8 * kc);
+#pragma unroll
+                for (int d = 0; d < NB; d++) o[d] = T::mfma(L::column_operand(vs, 16 * kc, d), p, o[d]);
             }
         }
-#pragma unroll
-        for (int i = 0; i < 32; i++) most = fmaxf(most, x[i]);
-        most = fmaxf(most, other_half(most));
-        const float m_new = fmaxf(m, most);
-        const float f = exp2_(m - m_new);
-        m = m_new;
-        l *= f;
-#pragma unroll
-        for (int d = 0; d < NB; d++) o[d] *= f;
-#pragma unroll
-        for (int i = 0; i < 32; i++) {
-            x[i] = exp2_(x[i] - m);
-            l += x[i];
+        if (t2 < w.t1) {
+            sk.store(tiles + (buf ^ 1) * SIZE);
+            sv.store(tiles + (2 + (buf ^ 1)) * SIZE);
         }
-#pragma unroll
-        for (int kc = 0; kc < 4; kc++) {
-            const s16x8 p = rounded<T>(x + 8 * kc);
-#pragma unroll
-            for (int d = 0; d < NB; d++) o[d] = T::mfma(L::column_operand(vs, 16 * kc, d), p, o[d]);
-        }
+        __syncthreads();
+        t = t2;
     }
     l += other_half(l);
-    if (row >= a.rows) return;
+    if (w.row >= a.rows) return;
     const bool nothing = l == 0;
     if (a.splits > 1) {
-        const int64_t at = ((int64_t)split * units + u.b * a.k_heads + u.g) * a.rows + row;
+        const int64_t at = ((int64_t)split * units + u.b * a.k_heads + u.g) * a.rows + w.row;
         float *po = a.part_out + at * a.head_dim;
 #pragma unroll
         for (int d = 0; d < NB; d++)
@@ -332,20 +436,16 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
         return;
     }
     const float inv = nothing ? 0.0f : 1.0f / l;
-    char *op = a.out.data + (u.b * a.out.batch + head * a.out.head + query * a.out.position) * 2;
 #pragma unroll
     for (int d = 0; d < NB; d++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int col = 32 * d + 8 * e + 4 * hi;
-            typedef R r4 __attribute__((ext_vector_type(4)));
-            r4 v;
-#pragma unroll
-            for (int i = 0; i < 4; i++) v[i] = (R)(nothing ? 0.0f : o[d][4 * e + i] * inv);
-            if (col < a.head_dim) *(r4 *)(op + col * 2) = v;
+            f32x4 v = {o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+            if (col < a.head_dim) write_out<T>(a, u.b, w.head, w.query, col, nothing ? f32x4{} : v * inv);
         }
     if (a.lse && hi == 0)
-        a.lse[((int64_t)u.b * a.k_heads * a.group + head) * a.q_len + query] =
+        a.lse[((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query] =
             nothing ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
@@ -353,7 +453,6 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
 template <typename T>
 __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
 {
-    using R = typename T::raw;
     const int64_t units = (int64_t)a.batch * a.k_heads, n = units * a.rows;
     const int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
     if (r >= n) return;
@@ -371,13 +470,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
     const int64_t unit = r / a.rows;
     const int row = (int)(r % a.rows), b = (int)(unit / a.k_heads), g = (int)(unit % a.k_heads);
     const int query = row / a.group, head = g * a.group + row % a.group;
-    if (c < a.head_dim) {
-        typedef R r4 __attribute__((ext_vector_type(4)));
-        r4 v;
-#pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = (R)(nothing ? 0.0f : o[i] / l);
-        *(r4 *)(a.out.data + (b * a.out.batch + head * a.out.head + query * a.out.position + c) * 2) = v;
-    }
+    if (c < a.head_dim) write_out<T>(a, b, head, query, c, nothing ? f32x4{} : o * (1.0f / l));
     if (a.lse && c == 0)
         a.lse[((int64_t)b * a.k_heads * a.group + head) * a.q_len + query] =
             nothing ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
@@ -408,72 +501,38 @@ __global__ void __launch_bounds__(256) row_stat_kernel(AttnArgs a)
     if (c < a.head_dim) {
         const r8 x = *(const r8 *)(head_base(a.out, b, head) + (query * a.out.position + c) * 2);
         const r8 y = *(const r8 *)(head_base(a.dout, b, head) + (query * a.dout.position + c) * 2);
+        r8 z = {};
+        if (a.rest) z = *(const r8 *)(a.rest + (((int64_t)b * a.q_len + query) * a.k_heads * a.group + head) * a.head_dim * 2 + c * 2);
 #pragma unroll
-        for (int i = 0; i < 8; i++) sum += (float)x[i] * (float)y[i];
+        for (int i = 0; i < 8; i++) sum += ((float)x[i] + (float)z[i]) * (float)y[i];
     }
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d);
     if (c == 0) {
-        const float lse = a.lse[((int64_t)b * a.k_heads * a.group + head) * a.q_len + query];
-        a.row_stat[r] = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, sum);
+        const int64_t at = ((int64_t)b * a.k_heads * a.group + head) * a.q_len + query;
+        const float lse = a.lse[at];
+        a.row_stat[at] = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, sum);
     }
 }
 
-template <typename T, int NB, bool CAP>
+template <typename T, int NB, bool SHAPED>
 __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
-    using R = typename T::raw;
-    __shared__ __align__(16) short ks[KEY_TILE * L::PITCH], vs[KEY_TILE * L::PITCH];
+    constexpr int SIZE = KEY_TILE * L::PITCH;
+    __shared__ __align__(16) short tiles[4 * SIZE];
     __shared__ int range[4];
 
     const int row_tiles = (a.rows + ROW_TILE - 1) / ROW_TILE;
     const int id = spread(blockIdx.x, gridDim.x);
-    const Unit u(a, id / row_tiles);
-    const int tile_row = (row_tiles - 1 - id % row_tiles) * ROW_TILE;
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, hi = lane / 32;
-    const int row = tile_row + wave * 32 + lane % 32, crow = min(row, a.rows - 1);
-    const int query = crow / a.group, head = u.g * a.group + crow % a.group;
-    const int pos = u.start + query;
-    const int p_first = u.start + tile_row / a.group, p_last = u.start + min(tile_row + ROW_TILE - 1, a.rows - 1) / a.group;
-    const bool has_doc = !u.docs || (pos >= 0 && pos < a.k_len);
-    const int doc = u.docs && has_doc ? u.docs[pos] : 0;
-    const int row_end = has_doc ? u.end(a, pos) : 0;
-
-    int t0 = 0, t1 = (u.end(a, p_last) + KEY_TILE - 1) / KEY_TILE, doc_lo = 0, doc_hi = 0;
-    bool one_doc = true;
-    if (u.docs) {
-        if (threadIdx.x == 0) {
-            range[0] = INT32_MAX;
-            range[1] = -1;
-            range[2] = INT32_MAX;
-            range[3] = INT32_MIN;
-        }
-        __syncthreads();
-        if (has_doc) {
-            atomicMin(&range[2], doc);
-            atomicMax(&range[3], doc);
-        }
-        one_doc = __syncthreads_and(has_doc);
-        doc_lo = range[2];
-        doc_hi = range[3];
-        for (int t = threadIdx.x; t < t1; t += 256) {
-            const int2 d = u.doc_tiles[t];
-            if (d.x <= doc_hi && d.y >= doc_lo) {
-                atomicMin(&range[0], t);
-                atomicMax(&range[1], t);
-            }
-        }
-        __syncthreads();
-        t0 = range[0];
-        t1 = range[1] + 1;
-        one_doc = one_doc && doc_lo == doc_hi;
-    }
+    const RowBlock w(a, id / row_tiles, (row_tiles - 1 - id % row_tiles) * ROW_TILE, range);
+    const Unit &u = w.u;
+    const int lane = threadIdx.x % WAVE, hi = lane / 32;
 
     s16x8 q[2 * NB], g[2 * NB];
     {
-        const char *qp = head_base(a.q, u.b, head) + query * a.q.position * 2;
-        const char *gp = head_base(a.dout, u.b, head) + query * a.dout.position * 2;
+        const char *qp = head_base(a.q, u.b, w.head) + w.query * a.q.position * 2;
+        const char *gp = head_base(a.dout, u.b, w.head) + w.query * a.dout.position * 2;
 #pragma unroll
         for (int s = 0; s < 2 * NB; s++) {
             const int d = 16 * s + 8 * hi;
@@ -481,100 +540,114 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
             g[s] = d < a.head_dim ? *(const s16x8 *)(gp + d * 2) : s16x8{};
         }
     }
-    const float2 stat = a.row_stat[(int64_t)(u.b * a.k_heads + u.g) * a.rows + crow];
-    const float slope2 = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
-    const float scale2 = CAP ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    const float2 stat = a.row_stat[((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query];
+    const bool capped = a.cap > 0, bias = a.slopes != nullptr;
+    const float slope2 = bias ? a.slopes[w.head] * LOG2E : 0.0f;
+    const float scale2 = capped ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
     f32x16 dq[NB] = {};
     const char *kb = head_base(a.k, u.b, u.g), *vb = head_base(a.v, u.b, u.g);
 
-    for (int t = t0; t < t1; t++) {
-        const int j0 = t * KEY_TILE;
-        bool in_doc = true;
-        if (u.docs) {
-            const int2 d = u.doc_tiles[t];
-            if (d.x > doc_hi || d.y < doc_lo) continue;
-            in_doc = one_doc && d.x == d.y;
-        }
-        Staged<NB, KEY_TILE> sk, sv;
-        sk.load(kb, a.k.position, j0, u.len, a.head_dim);
-        sv.load(vb, a.v.position, j0, u.len, a.head_dim);
-        __syncthreads();
-        sk.store(ks);
-        sv.store(vs);
-        __syncthreads();
-        const bool whole = in_doc && j0 + KEY_TILE <= u.end(a, p_first);
-#pragma unroll
-        for (int kbk = 0; kbk < 2; kbk++) {
-            f32x16 s = {}, dp = {};
-#pragma unroll
-            for (int st = 0; st < 2 * NB; st++) {
-                s = T::mfma(L::row_operand(ks, 32 * kbk + lane % 32, st), q[st], s);
-                dp = T::mfma(L::row_operand(vs, 32 * kbk + lane % 32, st), g[st], dp);
-            }
-            float x[16];
-            const float pf = (float)(pos - j0 - 32 * kbk - 4 * hi);
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const int c = 8 * (i / 4) + i % 4;
-                float v = s[i] * scale2, dcap = 1.0f;
-                if (CAP) {
-                    const float th = tanh_of(v);
-                    v = cap2 * th;
-                    dcap = 1.0f - th * th;
-                }
-                if (a.slopes) v -= slope2 * fabsf(pf - (float)c);
-                x[i] = exp2_(v - stat.x) * (dp[i] - stat.y) * dcap;
-            }
-            if (!whole) {
-#pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    const int j = j0 + 32 * kbk + 4 * hi + 8 * (i / 4) + i % 4;
-                    bool seen = j < row_end;
-                    if (u.docs) seen = seen && u.docs[min(j, a.k_len - 1)] == doc;
-                    x[i] = seen ? x[i] : 0.0f;
-                }
-            }
-#pragma unroll
-            for (int kc = 0; kc < 2; kc++) {
-                const s16x8 p = rounded<T>(x + 8 * kc);
-#pragma unroll
-                for (int d = 0; d < NB; d++) dq[d] = T::mfma(L::column_operand(ks, 32 * kbk + 16 * kc, d), p, dq[d]);
-            }
-        }
+    int t = w.next(w.t0);
+    Staged<NB> sk, sv;
+    if (t < w.t1) {
+        sk.load(kb, a.k.position, t * KEY_TILE, u.len, a.head_dim);
+        sv.load(vb, a.v.position, t * KEY_TILE, u.len, a.head_dim);
+        sk.store(tiles);
+        sv.store(tiles + 2 * SIZE);
     }
-    if (row >= a.rows) return;
-    char *op = a.dq.data + (u.b * a.dq.batch + head * a.dq.head + query * a.dq.position) * 2;
+    __syncthreads();
+    for (int buf = 0; t < w.t1; buf ^= 1) {
+        const int j0 = t * KEY_TILE, t2 = w.next(t + 1);
+        if (t2 < w.t1) {
+            sk.load(kb, a.k.position, t2 * KEY_TILE, u.len, a.head_dim);
+            sv.load(vb, a.v.position, t2 * KEY_TILE, u.len, a.head_dim);
+        }
+        if (j0 < w.wave_end) {
+            short *ks = tiles + buf * SIZE;
+            const short *vs = tiles + (2 + buf) * SIZE;
+            const bool whole = w.whole(t);
+#pragma unroll
+            for (int kb2 = 0; kb2 < 2; kb2++) {
+                f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int st = 0; st < 2 * NB; st++) {
+                    s = T::mfma(L::row_operand(ks, 32 * kb2 + lane % 32, st), q[st], s);
+                    dp = T::mfma(L::row_operand(vs, 32 * kb2 + lane % 32, st), g[st], dp);
+                }
+                float x[16], y[16];
+                if (SHAPED && capped) {
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        const float th = tanh_of(s[i] * scale2);
+                        y[i] = fmaf(cap2, th, -stat.x);
+                        x[i] = (dp[i] - stat.y) * fmaf(-th, th, 1.0f);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        y[i] = fmaf(s[i], scale2, -stat.x);
+                        x[i] = dp[i] - stat.y;
+                    }
+                }
+                if (SHAPED && bias) {
+                    const float pf = (float)(w.pos - j0 - 32 * kb2 - 4 * hi);
+#pragma unroll
+                    for (int i = 0; i < 16; i++) y[i] -= slope2 * fabsf(pf - (float)(8 * (i / 4) + i % 4));
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i++) x[i] *= exp2_(y[i]);
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < 16; i++)
+                        x[i] = w.sees(a, j0 + 32 * kb2 + 4 * hi + 8 * (i / 4) + i % 4) ? x[i] : 0.0f;
+                }
+#pragma unroll
+                for (int kc = 0; kc < 2; kc++) {
+                    const s16x8 p = rounded<T>(x + 8 * kc);
+#pragma unroll
+                    for (int d = 0; d < NB; d++) dq[d] = T::mfma(L::column_operand(ks, 32 * kb2 + 16 * kc, d), p, dq[d]);
+                }
+            }
+        }
+        if (t2 < w.t1) {
+            sk.store(tiles + (buf ^ 1) * SIZE);
+            sv.store(tiles + (2 + (buf ^ 1)) * SIZE);
+        }
+        __syncthreads();
+        t = t2;
+    }
+    if (w.row >= a.rows) return;
 #pragma unroll
     for (int d = 0; d < NB; d++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int col = 32 * d + 8 * e + 4 * hi;
-            typedef R r4 __attribute__((ext_vector_type(4)));
-            r4 v;
-#pragma unroll
-            for (int i = 0; i < 4; i++) v[i] = (R)(dq[d][4 * e + i] * a.scale);
-            if (col < a.head_dim) *(r4 *)(op + col * 2) = v;
+            const f32x4 v = {dq[d][4 * e], dq[d][4 * e + 1], dq[d][4 * e + 2], dq[d][4 * e + 3]};
+            if (col < a.head_dim) write_four<T>(a.dq, u.b, w.head, w.query, col, v * a.scale);
         }
 }
 
-constexpr int GRAD_KEYS = 128;    // keys of a workgroup
-constexpr int GRAD_ROWS = 32;     // rows of a step
-
-template <typename T, int NB, bool CAP>
+// A workgroup has 128 keys, a wavefront 32, and walks over steps of 64 queries
+// of one head after the other of the group (two buffers in LDS, one barrier a
+// step).  Where key blocks are few, the steps are cut into parts whose sums
+// are added up by grad_join_kernel.
+template <typename T, int NB, bool SHAPED>
 __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
-    using R = typename T::raw;
-    __shared__ __align__(16) short qs[GRAD_ROWS * L::PITCH], gs[GRAD_ROWS * L::PITCH];
-    __shared__ __align__(16) float lse2[GRAD_ROWS], delta[GRAD_ROWS], slopes2[GRAD_ROWS], posf[GRAD_ROWS];
-    __shared__ __align__(16) int end[GRAD_ROWS], rdoc[GRAD_ROWS];
+    constexpr int ROWS = STAGE_ROWS, SIZE = ROWS * L::PITCH;
+    __shared__ __align__(16) short tiles[4 * SIZE];     // two of Q, two of dout
+    __shared__ __align__(16) float lse2s[2][ROWS], deltas[2][ROWS];
+    __shared__ __align__(16) int docs[2][ROWS];
 
     const int key_blocks = (a.k_len + GRAD_KEYS - 1) / GRAD_KEYS;
-    const int id = spread(blockIdx.x, gridDim.x);
+    int id = spread(blockIdx.x, gridDim.x);
+    const int part = id % a.parts;
+    id /= a.parts;
     const Unit u(a, id / key_blocks);
     const int j0 = id % key_blocks * GRAD_KEYS;
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, hi = lane / 32;
-    const int key = j0 + wave * 32 + lane % 32;
+    const int lane = threadIdx.x % WAVE, hi = lane / 32;
+    const int jw = j0 + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) * 32, key = jw + lane % 32;
 
     s16x8 kf[2 * NB], vf[2 * NB];
     {
@@ -589,128 +662,183 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
         }
     }
     const int kdoc = u.docs ? u.docs[min(key, a.k_len - 1)] : 0;
-    const float scale2 = CAP ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    const bool capped = a.cap > 0, bias = a.slopes != nullptr;
+    const float scale2 = capped ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
     f32x16 dk[NB] = {}, dv[NB] = {};
 
-    // rows that may see any of the keys
-    int r0 = 0, r1 = j0 < u.len ? a.rows : 0, doc_lo = 0, doc_hi = 0;
-    if (a.causal && j0 >= u.prefix) r0 = (int)min((int64_t)max(j0 - u.start, 0) * a.group, (int64_t)a.rows) / GRAD_ROWS * GRAD_ROWS;
+    // queries that may see any of the keys: from `first` on, `tiles_q` steps a head
+    const int first = a.causal && j0 >= u.prefix ? min(max(j0 - u.start, 0), a.q_len) : 0;
+    const int tiles_q = j0 < u.len ? (a.q_len - first + ROWS - 1) / ROWS : 0;
+    int i0 = 0, i1 = tiles_q * a.group, doc_lo = 0, doc_hi = 0;
     if (u.docs) {
         const int2 d0 = u.doc_tiles[j0 / KEY_TILE], d1 = u.doc_tiles[min(j0 / KEY_TILE + 1, a.key_tiles - 1)];
         doc_lo = min(d0.x, d1.x);
         doc_hi = max(d0.y, d1.y);
     }
-    const float2 *stats = a.row_stat + (int64_t)(u.b * a.k_heads + u.g) * a.rows;
+    if (a.parts > 1) {
+        const int per = (i1 + a.parts - 1) / a.parts;
+        i0 = min(per * part, i1);
+        i1 = min(i0 + per, i1);
+    }
+    auto query_of = [&](int i) { return first + i % tiles_q * ROWS; };
+    // documents of a step's queries, as the (at most two) tiles of their positions give them
+    auto row_docs = [&](int q0) {
+        const int p0 = max(u.start + q0, 0), p1 = min(u.start + min(q0 + ROWS, a.q_len) - 1, a.k_len - 1);
+        if (p0 > p1) return make_int2(INT32_MAX, INT32_MIN);
+        const int2 x = u.doc_tiles[p0 / KEY_TILE], y = u.doc_tiles[p1 / KEY_TILE];
+        return make_int2(min(x.x, y.x), max(x.y, y.y));
+    };
+    auto next = [&](int i) {
+        if (u.docs)
+            for (; i < i1; i++) {
+                const int2 d = row_docs(query_of(i));
+                if (d.x <= doc_hi && d.y >= doc_lo) break;
+            }
+        return i;
+    };
+    Staged<NB> sq, sg;
+    float2 stat;
+    int rdoc = 0;
+    auto load = [&](int i) {
+        const int head = u.g * a.group + i / tiles_q, q0 = query_of(i);
+        sq.load(head_base(a.q, u.b, head), a.q.position, q0, a.q_len, a.head_dim);
+        sg.load(head_base(a.dout, u.b, head), a.dout.position, q0, a.q_len, a.head_dim);
+        if (threadIdx.x < ROWS) {
+            const int query = q0 + threadIdx.x, pos = u.start + query;
+            stat = query < a.q_len ? a.row_stat[((int64_t)u.b * a.k_heads * a.group + head) * a.q_len + query]
+                                   : make_float2(INFINITY, 0.0f);
+            if (u.docs) {
+                // a position without a document sees nothing
+                if (pos >= 0 && pos < a.k_len) rdoc = u.docs[pos];
+                else stat.x = INFINITY;
+            }
+        }
+    };
+    auto store = [&](int buf) {
+        sq.store(tiles + buf * SIZE);
+        sg.store(tiles + (2 + buf) * SIZE);
+        if (threadIdx.x < ROWS) {
+            lse2s[buf][threadIdx.x] = stat.x - T::p_shift;
+            deltas[buf][threadIdx.x] = stat.y * (1.0f / T::p_gain);
+            docs[buf][threadIdx.x] = rdoc;
+        }
+    };
 
-    for (int rr = r0; rr < r1; rr += GRAD_ROWS) {
-        const int p_first = u.start + rr / a.group, p_last = u.start + min(rr + GRAD_ROWS - 1, a.rows - 1) / a.group;
+    int i = next(i0);
+    if (i < i1) {
+        load(i);
+        store(0);
+    }
+    __syncthreads();
+    for (int buf = 0; i < i1; buf ^= 1) {
+        const int i2 = next(i + 1), q0 = query_of(i);
+        if (i2 < i1) load(i2);
         bool in_doc = true;
         if (u.docs) {
-            if (p_last < 0 || p_first >= a.k_len) continue;
-            const int2 d0 = u.doc_tiles[max(p_first, 0) / KEY_TILE], d1 = u.doc_tiles[min(p_last, a.k_len - 1) / KEY_TILE];
-            bool overlap = false;
-            int lo = min(d0.x, d1.x), hi2 = max(d0.y, d1.y);
-            for (int t = max(p_first, 0) / KEY_TILE + 1; t < min(p_last, a.k_len - 1) / KEY_TILE; t++) {
-                const int2 d = u.doc_tiles[t];
-                lo = min(lo, d.x);
-                hi2 = max(hi2, d.y);
-            }
-            overlap = lo <= doc_hi && hi2 >= doc_lo;
-            if (!overlap) continue;
-            in_doc = lo == hi2 && doc_lo == doc_hi && p_first >= 0 && p_last < a.k_len;
+            const int2 d = row_docs(q0);
+            in_doc = d.x == d.y && doc_lo == doc_hi && u.start + q0 >= 0 && u.start + min(q0 + ROWS, a.q_len) <= a.k_len;
         }
-        __syncthreads();
-        {
-            constexpr int N = GRAD_ROWS * L::CHUNKS / 256;
-            const int c = threadIdx.x % L::CHUNKS;
+        const float slope2 = SHAPED && bias ? a.slopes[u.g * a.group + i / tiles_q] * LOG2E : 0.0f;
+#pragma unroll 1
+        for (int sb = 0; sb < 2; sb++) {
+            const int qs0 = q0 + 32 * sb, p0 = u.start + qs0;                  // the first of 32 queries
+            if (qs0 >= a.q_len || jw >= u.end(a, p0 + 31)) continue;
+            const bool whole = in_doc && jw + 32 <= u.end(a, p0);
+            short *qt = tiles + buf * SIZE + 32 * sb * L::PITCH, *gt = tiles + (2 + buf) * SIZE + 32 * sb * L::PITCH;
+            f32x16 s = {}, dp = {};
 #pragma unroll
-            for (int n = 0; n < N; n++) {
-                const int i = threadIdx.x / L::CHUNKS + n * (256 / L::CHUNKS), r = rr + i;
-                const int query = r / a.group, head = u.g * a.group + r % a.group;
-                uint4 x = make_uint4(0, 0, 0, 0), y = x;
-                if (r < a.rows && c * 8 < a.head_dim) {
-                    x = *(const uint4 *)(head_base(a.q, u.b, head) + (query * a.q.position + c * 8) * 2);
-                    y = *(const uint4 *)(head_base(a.dout, u.b, head) + (query * a.dout.position + c * 8) * 2);
+            for (int st = 0; st < 2 * NB; st++) {
+                s = T::mfma(L::row_operand(qt, lane % 32, st), kf[st], s);
+                dp = T::mfma(L::row_operand(gt, lane % 32, st), vf[st], dp);
+            }
+            float p[16], ds[16];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const f32x4 lse2 = *(const f32x4 *)&lse2s[buf][32 * sb + 8 * e + 4 * hi];
+                const f32x4 delta = *(const f32x4 *)&deltas[buf][32 * sb + 8 * e + 4 * hi];
+                if (SHAPED && capped) {
+#pragma unroll
+                    for (int n = 0; n < 4; n++) {
+                        const float th = tanh_of(s[4 * e + n] * scale2);
+                        p[4 * e + n] = fmaf(cap2, th, -lse2[n]);
+                        ds[4 * e + n] = fmaf(dp[4 * e + n], 1.0f / T::p_gain, -delta[n]) * fmaf(-th, th, 1.0f);
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < 4; n++) {
+                        p[4 * e + n] = fmaf(s[4 * e + n], scale2, -lse2[n]);
+                        ds[4 * e + n] = fmaf(dp[4 * e + n], 1.0f / T::p_gain, -delta[n]);
+                    }
                 }
-                *(uint4 *)(qs + L::at(i, c)) = x;
-                *(uint4 *)(gs + L::at(i, c)) = y;
             }
-            if (threadIdx.x < GRAD_ROWS) {
-                const int i = threadIdx.x, r = rr + i, query = r / a.group, pos = u.start + query;
-                const bool in = r < a.rows, has_doc = !u.docs || (pos >= 0 && pos < a.k_len);
-                const float2 st = in ? stats[r] : make_float2(INFINITY, 0.0f);
-                lse2[i] = st.x;
-                delta[i] = st.y / T::p_gain;
-                slopes2[i] = a.slopes && in ? a.slopes[u.g * a.group + r % a.group] * LOG2E : 0.0f;
-                posf[i] = (float)pos;
-                end[i] = in && has_doc ? u.end(a, pos) : 0;
-                rdoc[i] = in && u.docs && has_doc ? u.docs[pos] : 0;
+            if (SHAPED && bias) {
+                const float kf0 = (float)(key - p0 - 4 * hi);
+#pragma unroll
+                for (int n = 0; n < 16; n++) p[n] -= slope2 * fabsf(kf0 - (float)(8 * (n / 4) + n % 4));
+            }
+#pragma unroll
+            for (int n = 0; n < 16; n++) {
+                p[n] = exp2_(p[n]);
+                ds[n] *= p[n];
+            }
+            if (!whole) {
+                // queries of the 32 that see the key: from `from` on
+                const int from = key >= u.len ? INT32_MAX : a.causal && key >= u.prefix ? key - p0 - 4 * hi : INT32_MIN;
+#pragma unroll
+                for (int n = 0; n < 16; n++) {
+                    const int r = 8 * (n / 4) + n % 4;
+                    const bool seen = r >= from && (!u.docs || docs[buf][32 * sb + 4 * hi + r] == kdoc);
+                    p[n] = seen ? p[n] : 0.0f;
+                    ds[n] = seen ? ds[n] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int kc = 0; kc < 2; kc++) {
+                const s16x8 pr = rounded<T>(p + 8 * kc), dr = rounded<T>(ds + 8 * kc);
+#pragma unroll
+                for (int d = 0; d < NB; d++) {
+                    dv[d] = T::mfma(L::column_operand(gt, 16 * kc, d), pr, dv[d]);
+                    dk[d] = T::mfma(L::column_operand(qt, 16 * kc, d), dr, dk[d]);
+                }
             }
         }
+        if (i2 < i1) store(buf ^ 1);
         __syncthreads();
-        const bool whole = in_doc && j0 + GRAD_KEYS <= u.end(a, p_first);
-
-        f32x16 s = {}, dp = {};
-#pragma unroll
-        for (int st = 0; st < 2 * NB; st++) {
-            s = T::mfma(L::row_operand(qs, lane % 32, st), kf[st], s);
-            dp = T::mfma(L::row_operand(gs, lane % 32, st), vf[st], dp);
-        }
-        float p[16], ds[16];
-        const float keyf = (float)key;
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const int r = 8 * (i / 4) + 4 * hi + i % 4;
-            float v = s[i] * scale2, dcap = 1.0f;
-            if (CAP) {
-                const float th = tanh_of(v);
-                v = cap2 * th;
-                dcap = 1.0f - th * th;
-            }
-            if (a.slopes) v -= slopes2[r] * fabsf(posf[r] - keyf);
-            p[i] = exp2_(v - lse2[r]) * T::p_gain;
-            ds[i] = p[i] * (dp[i] * (1.0f / T::p_gain) - delta[r]) * dcap;
-        }
-        if (!whole) {
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const int r = 8 * (i / 4) + 4 * hi + i % 4;
-                bool seen = key < end[r];
-                if (u.docs) seen = seen && rdoc[r] == kdoc;
-                p[i] = seen ? p[i] : 0.0f;
-                ds[i] = seen ? ds[i] : 0.0f;
-            }
-        }
-#pragma unroll
-        for (int kc = 0; kc < 2; kc++) {
-            const s16x8 pr = rounded<T>(p + 8 * kc), dr = rounded<T>(ds + 8 * kc);
-#pragma unroll
-            for (int d = 0; d < NB; d++) {
-                dv[d] = T::mfma(L::column_operand(gs, 16 * kc, d), pr, dv[d]);
-                dk[d] = T::mfma(L::column_operand(qs, 16 * kc, d), dr, dk[d]);
-            }
-        }
+        i = i2;
     }
     if (key >= a.k_len) return;
-    char *kp = a.dk.data + (u.b * a.dk.batch + u.g * a.dk.head + key * a.dk.position) * 2;
-    char *vp = a.dv.data + (u.b * a.dv.batch + u.g * a.dv.head + key * a.dv.position) * 2;
+    const int64_t units = (int64_t)a.batch * a.k_heads;
+    float *part_k = a.part_grad + (((int64_t)part * 2 * units + u.b * a.k_heads + u.g) * a.k_len + key) * a.head_dim;
+    float *part_v = part_k + units * a.k_len * a.head_dim;
 #pragma unroll
     for (int d = 0; d < NB; d++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int col = 32 * d + 8 * e + 4 * hi;
-            typedef R r4 __attribute__((ext_vector_type(4)));
-            r4 x, y;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                x[i] = (R)(dk[d][4 * e + i] * a.scale);
-                y[i] = (R)(dv[d][4 * e + i] * (1.0f / T::p_gain));
-            }
-            if (col < a.head_dim) {
-                *(r4 *)(kp + col * 2) = x;
-                *(r4 *)(vp + col * 2) = y;
+            const f32x4 x = f32x4{dk[d][4 * e], dk[d][4 * e + 1], dk[d][4 * e + 2], dk[d][4 * e + 3]} * a.scale;
+            const f32x4 y = f32x4{dv[d][4 * e], dv[d][4 * e + 1], dv[d][4 * e + 2], dv[d][4 * e + 3]} * (1.0f / T::p_gain);
+            if (col >= a.head_dim) continue;
+            if (a.parts > 1) {
+                *(f32x4 *)(part_k + col) = x;
+                *(f32x4 *)(part_v + col) = y;
+            } else {
+                write_four<T>(a.dk, u.b, u.g, key, col, x);
+                write_four<T>(a.dv, u.b, u.g, key, col, y);
             }
         }
+}
+
+// Adds up the parts of dK (blockIdx.y 0) and dV (1): 8 keys a workgroup, four columns a lane.
+template <typename T>
+__global__ void __launch_bounds__(256) grad_join_kernel(AttnArgs a)
+{
+    const int64_t n = (int64_t)a.batch * a.k_heads * a.k_len, r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    const int c = threadIdx.x % 32 * 4;
+    if (r >= n || c >= a.head_dim) return;
+    f32x4 sum = {};
+    for (int p = 0; p < a.parts; p++) sum += *(const f32x4 *)(a.part_grad + ((2 * p + blockIdx.y) * n + r) * a.head_dim + c);
+    const int64_t unit = r / a.k_len;
+    write_four<T>(blockIdx.y ? a.dv : a.dk, (int)(unit / a.k_heads), (int)(unit % a.k_heads), r % a.k_len, c, sum);
 }
 
 hipError_t doc_tiles(const AttnArgs &a, hipStream_t st)
@@ -720,11 +848,11 @@ hipError_t doc_tiles(const AttnArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-template <typename T, int NB, bool CAP> hipError_t forward_sized(const AttnArgs &a, hipStream_t st)
+template <typename T, int NB, bool SHAPED> hipError_t forward_sized(const AttnArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
     const unsigned n = (unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE) * a.splits);
-    forward_kernel<T, NB, CAP><<<n, 256, 0, st>>>(a);
+    forward_kernel<T, NB, SHAPED><<<n, 256, 0, st>>>(a);
     if (a.splits > 1) {
         if (hipError_t e = hipGetLastError()) return e;
         join_kernel<T><<<(unsigned)((units * a.rows + 7) / 8), 256, 0, st>>>(a);
@@ -732,29 +860,35 @@ template <typename T, int NB, bool CAP> hipError_t forward_sized(const AttnArgs 
     return hipGetLastError();
 }
 
-template <typename T, int NB, bool CAP> hipError_t backward_sized(const AttnArgs &a, hipStream_t st)
+template <typename T, int NB, bool SHAPED> hipError_t backward_sized(const AttnArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
     if (a.rows) {
         row_stat_kernel<T><<<(unsigned)((units * a.rows + 15) / 16), 256, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
-        dq_kernel<T, NB, CAP><<<(unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE)), 256, 0, st>>>(a);
+        dq_kernel<T, NB, SHAPED><<<(unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE)), 256, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    if (a.k_len) dkv_kernel<T, NB, CAP><<<(unsigned)(units * ((a.k_len + GRAD_KEYS - 1) / GRAD_KEYS)), 256, 0, st>>>(a);
+    if (a.k_len) {
+        dkv_kernel<T, NB, SHAPED><<<(unsigned)(units * ((a.k_len + GRAD_KEYS - 1) / GRAD_KEYS) * a.parts), 256, 0, st>>>(a);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (a.parts > 1) grad_join_kernel<T><<<dim3((unsigned)((units * a.k_len + 7) / 8), 2), 256, 0, st>>>(a);
+    }
     return hipGetLastError();
 }
 
 template <typename T> hipError_t forward_typed(const AttnArgs &a, hipStream_t st)
 {
-    if (a.head_dim <= 64) return a.cap > 0 ? forward_sized<T, 2, true>(a, st) : forward_sized<T, 2, false>(a, st);
-    return a.cap > 0 ? forward_sized<T, 4, true>(a, st) : forward_sized<T, 4, false>(a, st);
+    const bool shaped = a.cap > 0 || a.slopes;
+    if (a.head_dim <= 64) return shaped ? forward_sized<T, 2, true>(a, st) : forward_sized<T, 2, false>(a, st);
+    return shaped ? forward_sized<T, 4, true>(a, st) : forward_sized<T, 4, false>(a, st);
 }
 
 template <typename T> hipError_t backward_typed(const AttnArgs &a, hipStream_t st)
 {
-    if (a.head_dim <= 64) return a.cap > 0 ? backward_sized<T, 2, true>(a, st) : backward_sized<T, 2, false>(a, st);
-    return a.cap > 0 ? backward_sized<T, 4, true>(a, st) : backward_sized<T, 4, false>(a, st);
+    const bool shaped = a.cap > 0 || a.slopes;
+    if (a.head_dim <= 64) return shaped ? backward_sized<T, 2, true>(a, st) : backward_sized<T, 2, false>(a, st);
+    return shaped ? backward_sized<T, 4, true>(a, st) : backward_sized<T, 4, false>(a, st);
 }
 
 }  // namespace

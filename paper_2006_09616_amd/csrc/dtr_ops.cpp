@@ -16,6 +16,7 @@ using namespace dtrops;
 namespace {
 
 constexpr int32_t MAX_LEN = 1 << 24;
+constexpr int64_t MAX_STRIDE = int64_t(1) << 26; // between positions: 32-bit offsets within 16 of them
 constexpr int64_t MAX_ROWS = int64_t(1) << 31;
 constexpr int64_t MAX_GROUPS = int64_t(1) << 24;   // workgroups of a launch: 2^32 work items
 
@@ -53,6 +54,8 @@ int check_heads(const char *name, const dtr_heads *t, const dtr_attn *a, bool ou
     if (!t->data) return fail(DTR_EINVAL, "attention: null %s", name);
     if ((uintptr_t)t->data % 16 || t->batch % 8 || t->position % 8 || t->head % 8)
         return fail(DTR_EINVAL, "attention: rows of %s do not start at multiples of 16 bytes", name);
+    if (len > 1 && t->position >= MAX_STRIDE)
+        return fail(DTR_EINVAL, "attention: positions of %s are %lld elements apart", name, (long long)t->position);
     if (t->batch < 0 || t->position < 0 || t->head < 0) return fail(DTR_EINVAL, "attention: negative stride of %s", name);
     if (output && ((a->batch > 1 && t->batch == 0) || (len > 1 && t->position == 0) || (heads > 1 && t->head == 0)))
         return fail(DTR_EINVAL, "attention: %s overlaps itself", name);
@@ -60,8 +63,8 @@ int check_heads(const char *name, const dtr_heads *t, const dtr_attn *a, bool ou
 }
 
 struct Plan {
-    int32_t splits;
-    size_t docs, part_out, part_stat, row_stat, total;
+    int32_t splits, parts;
+    size_t docs, part_out, part_stat, part_grad, row_stat, total;
 };
 
 // Parts that the keys are split into.  One part per row tile leaves most of
@@ -72,6 +75,16 @@ int32_t splits_for(int64_t tiles, int64_t key_tiles)
     if (tiles >= 256 || key_tiles < 8) return 1;
     const int64_t want = (512 + tiles - 1) / tiles;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(want, key_tiles / 4), 256));
+}
+
+// Parts that the rows are cut into for dK and dV.  A key block's work ranges
+// from none to all rows under a causal mask, so that a card of 256 compute
+// units wants several blocks for each; a part of fewer than 512 rows would
+// spend its time on the 32-bit partial sums.
+int32_t parts_for(int64_t blocks, int64_t rows)
+{
+    if (blocks >= 1024) return 1;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((1024 + blocks - 1) / std::max<int64_t>(blocks, 1), rows / 512), 16));
 }
 
 Plan make_plan(const dtr_attn *a, bool backward)
@@ -91,7 +104,12 @@ Plan make_plan(const dtr_attn *a, bool backward)
         p.part_out = take(sizeof(float) * p.splits * units * rows * a->head_dim);
         p.part_stat = take(sizeof(float2) * p.splits * units * rows);
     }
-    if (backward) p.row_stat = take(sizeof(float2) * units * rows);
+    p.parts = 1;
+    if (backward) {
+        p.parts = parts_for(units * ((a->k_len + GRAD_KEYS - 1) / GRAD_KEYS), rows);
+        p.row_stat = take(sizeof(float2) * units * rows);
+        if (p.parts > 1) p.part_grad = take(sizeof(float) * 2 * p.parts * units * a->k_len * a->head_dim);
+    }
     p.total = at;
     return p;
 }
@@ -117,6 +135,8 @@ AttnArgs make_args(const dtr_attn *a, const Plan &p, char *ws)
     k.starts = a->starts;
     k.rows = (int32_t)((int64_t)a->q_len * k.group);
     k.splits = p.splits;
+    k.parts = p.parts;
+    k.part_grad = (float *)(ws + p.part_grad);
     k.key_tiles = (a->k_len + KEY_TILE - 1) / KEY_TILE;
     k.doc_tiles = (int2 *)(ws + p.docs);
     k.part_out = (float *)(ws + p.part_out);
@@ -180,7 +200,7 @@ int dtr_attn_workspace_bytes(const dtr_attn *attn, int32_t backward, size_t *byt
 }
 
 int dtr_attn_forward(const dtr_attn *attn, const dtr_heads *q, const dtr_heads *k, const dtr_heads *v,
-                     const dtr_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+                     const dtr_heads *out, void *rest, float *lse, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (int rc = check_attn(attn)) return rc;
     if (int rc = check_heads("q", q, attn, false)) return rc;
@@ -195,13 +215,16 @@ int dtr_attn_forward(const dtr_attn *attn, const dtr_heads *q, const dtr_heads *
     a.k = of(k);
     a.v = of(v);
     a.out = of(out);
+    if ((uintptr_t)rest % 16) return fail(DTR_EINVAL, "attention: rest is not 16-byte aligned");
+    a.rest = (char *)rest;
     a.lse = lse;
     return launched(launch_attn_forward(a, attn->type, (hipStream_t)stream), "attention forward");
 }
 
 int dtr_attn_backward(const dtr_attn *attn, const dtr_heads *q, const dtr_heads *k, const dtr_heads *v,
-                      const dtr_heads *out, const float *lse, const dtr_heads *dout, const dtr_heads *dq,
-                      const dtr_heads *dk, const dtr_heads *dv, void *workspace, size_t workspace_bytes, void *stream)
+                      const dtr_heads *out, const void *rest, const float *lse, const dtr_heads *dout,
+                      const dtr_heads *dq, const dtr_heads *dk, const dtr_heads *dv, void *workspace,
+                      size_t workspace_bytes, void *stream)
 {
     if (int rc = check_attn(attn)) return rc;
     if (int rc = check_heads("q", q, attn, false)) return rc;
@@ -221,6 +244,8 @@ int dtr_attn_backward(const dtr_attn *attn, const dtr_heads *q, const dtr_heads 
     a.k = of(k);
     a.v = of(v);
     a.out = of(out);
+    if ((uintptr_t)rest % 16) return fail(DTR_EINVAL, "attention: rest is not 16-byte aligned");
+    a.rest = (char *)rest;
     a.dout = of(dout);
     a.dq = of(dq);
     a.dk = of(dk);

@@ -11,6 +11,7 @@ namespace dtrops {
 
 constexpr int KEY_TILE = 64;      // keys of a tile of the attention kernels
 constexpr int ROW_TILE = 128;     // rows (queries x heads of a group) of a workgroup
+constexpr int GRAD_KEYS = 128;    // keys of a workgroup that sums dK and dV
 constexpr int SEGS = 4;           // segments of a row that a workgroup of the log-probability kernel reads
 
 struct Heads {                    // [batch][position][head][head_dim], strides in elements
@@ -24,6 +25,7 @@ struct AttnArgs {
     const float *slopes;
     const int32_t *prefix, *docs, *lengths, *starts;
     Heads q, k, v, out, dout, dq, dk, dv;
+    char *rest;                   // [batch][q_len][q_heads][head_dim] what rounding took from out, or NULL
     float *lse;                   // [batch][q_heads][q_len]
     int32_t rows;                 // q_len * group: rows of one key head, row = query * group + head of the group
     int32_t splits;               // parts that the keys are split into (forward)
@@ -31,7 +33,9 @@ struct AttnArgs {
     int2 *doc_tiles;              // [batch][key_tiles] smallest and largest document of each tile
     float *part_out;              // [splits][batch][k_heads][rows][head_dim] (splits > 1)
     float2 *part_stat;            // [splits][batch][k_heads][rows] maximum and sum
-    float2 *row_stat;             // [batch][k_heads][rows] log2-sum-exp2 and out.dout (backward)
+    int32_t parts;                // parts that the rows are cut into (dK and dV)
+    float *part_grad;             // [parts][2][batch][k_heads][k_len][head_dim] (parts > 1)
+    float2 *row_stat;             // [batch][q_heads][q_len] log2-sum-exp2 and out . dout (backward)
 };
 
 struct LogpArgs {

@@ -25,6 +25,7 @@ from . import dtr
 HEADER = os.path.join(os.path.dirname(dtr.HERE), "include", "dtr_ops.h")
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 TOP_MAX = 32
+MAX_STRIDE = 1 << 26
 
 
 class _Attn(C.Structure):
@@ -47,8 +48,8 @@ def lib():
     if not _ready:
         vp, i32, i64, sz, u64 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_uint64
         L.dtr_attn_workspace_bytes.argtypes = [vp, i32, vp]
-        L.dtr_attn_forward.argtypes = [vp] * 7 + [sz, vp]
-        L.dtr_attn_backward.argtypes = [vp] * 11 + [sz, vp]
+        L.dtr_attn_forward.argtypes = [vp] * 8 + [sz, vp]
+        L.dtr_attn_backward.argtypes = [vp] * 12 + [sz, vp]
         L.dtr_dropout_add.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, i64, C.c_double, u64, u64, vp]
         L.dtr_logprobs_workspace_bytes.argtypes = [i32, i64, i64, i32, vp]
         L.dtr_logprobs_forward.argtypes = [i32, i64, i64, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -97,7 +98,8 @@ def _int32(name: str, t, shape, device):
 def _rows(t: torch.Tensor) -> torch.Tensor:
     """t itself where its rows can be read in 16-byte pieces, else a copy."""
     ok = t.numel() == 0 or (t.stride(3) == 1 and t.data_ptr() % 16 == 0 and
-                            all(t.stride(d) % 8 == 0 or t.shape[d] == 1 for d in range(3)))
+                            all(t.stride(d) % 8 == 0 or t.shape[d] == 1 for d in range(3)) and
+                            (t.stride(1) < MAX_STRIDE or t.shape[1] == 1))
     return t if ok else t.contiguous()
 
 
@@ -115,22 +117,23 @@ def _record(q, k, opts) -> _Attn:
                  *(_ptr(opts[n]) for n in ("slopes", "prefix", "docs", "lengths", "starts")))
 
 
-def _attn_forward(q, k, v, opts, want_lse: bool):
+def _attn_forward(q, k, v, opts, want_lse: bool, want_rest: bool = False):
     L = lib()
     with torch.cuda.device(q.device):
         q, k, v = _rows(q), _rows(k), _rows(v)
         rec = _record(q, k, opts)
         out = _like(q)
         lse = torch.empty(q.shape[0], q.shape[2], q.shape[1], dtype=torch.float32, device=q.device) if want_lse else None
+        rest = _like(q) if want_rest else None
         n = C.c_size_t(0)
         dtr._check(L.dtr_attn_workspace_bytes(C.byref(rec), 0, C.byref(n)))
         ws = _workspace(n.value, q.device)
         dtr._check(L.dtr_attn_forward(C.byref(rec), C.byref(_heads(q)), C.byref(_heads(k)), C.byref(_heads(v)),
-                                      C.byref(_heads(out)), _ptr(lse), _ptr(ws), n.value, _stream(q.device)))
-    return out, lse
+                                      C.byref(_heads(out)), _ptr(rest), _ptr(lse), _ptr(ws), n.value, _stream(q.device)))
+    return out, lse, rest
 
 
-def _attn_backward(q, k, v, out, lse, dout, opts):
+def _attn_backward(q, k, v, out, rest, lse, dout, opts):
     L = lib()
     with torch.cuda.device(q.device):
         q, k, v, out, dout = _rows(q), _rows(k), _rows(v), _rows(out), _rows(dout)
@@ -139,7 +142,7 @@ def _attn_backward(q, k, v, out, lse, dout, opts):
         n = C.c_size_t(0)
         dtr._check(L.dtr_attn_workspace_bytes(C.byref(rec), 1, C.byref(n)))
         ws = _workspace(n.value, q.device)
-        dtr._check(L.dtr_attn_backward(C.byref(rec), *(C.byref(_heads(t)) for t in (q, k, v, out)), _ptr(lse),
+        dtr._check(L.dtr_attn_backward(C.byref(rec), *(C.byref(_heads(t)) for t in (q, k, v, out)), _ptr(rest), _ptr(lse),
                                        *(C.byref(_heads(t)) for t in (dout, dq, dk, dv)), _ptr(ws), n.value,
                                        _stream(q.device)))
     return dq, dk, dv
@@ -148,8 +151,8 @@ def _attn_backward(q, k, v, out, lse, dout, opts):
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, opts):
-        out, lse = _attn_forward(q, k, v, opts, True)
-        ctx.save_for_backward(q, k, v, out, lse)
+        out, lse, rest = _attn_forward(q, k, v, opts, True, True)
+        ctx.save_for_backward(q, k, v, out, lse, rest)
         ctx.opts = opts
         ctx.mark_non_differentiable(lse)
         return out, lse
@@ -157,8 +160,8 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout, _):
-        q, k, v, out, lse = ctx.saved_tensors
-        return (*_attn_backward(q, k, v, out, lse, dout, ctx.opts), None)
+        q, k, v, out, lse, rest = ctx.saved_tensors
+        return (*_attn_backward(q, k, v, out, rest, lse, dout, ctx.opts), None)
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, scale: Optional[float] = None, cap: float = 0.0,
@@ -207,7 +210,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, scale: Optio
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         out, lse = _Attention.apply(q, k, v, opts)
     else:
-        out, lse = _attn_forward(q, k, v, opts, return_lse)
+        out, lse, _ = _attn_forward(q, k, v, opts, return_lse)
     return (out, lse) if return_lse else out
 
 
