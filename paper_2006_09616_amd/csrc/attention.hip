@@ -208,9 +208,9 @@ __device__ __forceinline__ void write_out(const AttnArgs &a, int b, int head, in
     }
 }
 
-// The rows of a workgroup (32 a wavefront, one a lane pair) and the tiles of
-// keys that any of them may see.
-struct RowBlock {
+// The rows of a workgroup (ROWS from tile_row on; `mine` is the lane's, with
+// 31 others in its wavefront) and the tiles of keys that any of them may see.
+template <int ROWS, int THREADS> struct RowBlock {
     Unit u;
     int row, query, head, pos, doc, end;     // of the lane's row; keys from `end` on are masked for it
     int sure;                                // keys before `sure` are seen by all rows, but for documents
@@ -219,10 +219,10 @@ struct RowBlock {
     int doc_lo, doc_hi;
     bool one_doc;
 
-    __device__ RowBlock(const AttnArgs &a, int unit, int tile_row, int (&range)[4]) : u(a, unit)
+    __device__ RowBlock(const AttnArgs &a, int unit, int tile_row, int mine, int (&range)[4]) : u(a, unit)
     {
-        const int wave = threadIdx.x / WAVE, last = a.rows - 1;
-        row = tile_row + wave * 32 + threadIdx.x % 32;
+        const int last = a.rows - 1;
+        row = mine;
         const int r = min(row, last);
         query = r / a.group;
         head = u.g * a.group + r % a.group;
@@ -231,9 +231,9 @@ struct RowBlock {
         doc = u.docs && has_doc ? u.docs[pos] : 0;
         end = has_doc ? u.end(a, pos) : 0;
         sure = u.end(a, u.start + tile_row / a.group);
-        wave_end = u.end(a, u.start + min(tile_row + wave * 32 + 31, last) / a.group);
+        wave_end = u.end(a, u.start + min(__builtin_amdgcn_readfirstlane(mine) + 31, last) / a.group);
         t0 = 0;
-        t1 = (u.end(a, u.start + min(tile_row + ROW_TILE - 1, last) / a.group) + KEY_TILE - 1) / KEY_TILE;
+        t1 = (u.end(a, u.start + min(tile_row + ROWS - 1, last) / a.group) + KEY_TILE - 1) / KEY_TILE;
         doc_lo = doc_hi = 0;
         one_doc = true;
         if (!u.docs) return;
@@ -251,7 +251,7 @@ struct RowBlock {
         one_doc = __syncthreads_and(has_doc);
         doc_lo = __builtin_amdgcn_readfirstlane(range[2]);
         doc_hi = __builtin_amdgcn_readfirstlane(range[3]);
-        for (int t = threadIdx.x; t < t1; t += 256)
+        for (int t = threadIdx.x; t < t1; t += THREADS)
             if (near(t)) {
                 atomicMin(&range[0], t);
                 atomicMax(&range[1], t);
@@ -289,6 +289,36 @@ struct RowBlock {
     }
 };
 
+// The scores of a lane's keys (key0 + 4 (lane / 32) + 32 (i / 16) + 8 (i % 16 / 4)
+// + i % 4), shaped in place: times log2(e), capped, biased.
+struct Shape {
+    bool capped, bias;
+    float scale2, cap2, slope2;
+    __device__ Shape(const AttnArgs &a, int head)
+    {
+        capped = a.cap > 0;
+        bias = a.slopes != nullptr;
+        slope2 = bias ? a.slopes[head] * LOG2E : 0.0f;
+        scale2 = capped ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E;
+        cap2 = a.cap * LOG2E;
+    }
+    template <int N> __device__ void apply(float (&x)[N], int distance0) const
+    {
+        if (capped) {
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = cap2 * tanh_of(x[i] * scale2);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] *= scale2;
+        }
+        if (bias) {
+            const float pf = (float)distance0;
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] -= slope2 * fabsf(pf - (float)(32 * (i / 16) + 8 * (i % 16 / 4) + i % 4));
+        }
+    }
+};
+
 // ---- forward -----------------------------------------------------------------
 // A workgroup has 128 rows, a wavefront 32, and walks over tiles of 64 keys.
 // The next tile is on its way from memory to registers while one is worked
@@ -309,7 +339,8 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
     const int split = id % a.splits;
     id /= a.splits;
     // the longest first under a causal mask
-    RowBlock w(a, id / row_tiles, (row_tiles - 1 - id % row_tiles) * ROW_TILE, range);
+    const int tile_row = (row_tiles - 1 - id % row_tiles) * ROW_TILE;
+    RowBlock<ROW_TILE, 256> w(a, id / row_tiles, tile_row, tile_row + threadIdx.x / WAVE * 32 + threadIdx.x % 32, range);
     if (a.splits > 1) {                                  // this part's tiles
         const int n = max(w.t1 - w.t0, 0), per = (n + a.splits - 1) / a.splits;
         w.t0 = min(w.t0, w.t1) + per * split;
@@ -327,9 +358,7 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
             q[s] = d < a.head_dim ? *(const s16x8 *)(qp + d * 2) : s16x8{};
         }
     }
-    const bool capped = a.cap > 0, bias = a.slopes != nullptr;
-    const float slope2 = bias ? a.slopes[w.head] * LOG2E : 0.0f;
-    const float scale2 = capped ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    const Shape shape(a, w.head);
 
     f32x16 o[NB] = {};
     float m = LOWEST, l = 0;
@@ -361,26 +390,10 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
                     s[kb2] = T::mfma(L::row_operand(ks, 32 * kb2 + lane % 32, st), q[st], s[kb2]);
             // x: the scores times log2(e); plain ones but for a factor left to the exponent's fma
             float x[32];
-            const float gain = SHAPED ? 1.0f : scale2;
+            const float gain = SHAPED ? 1.0f : shape.scale2;
 #pragma unroll
             for (int i = 0; i < 32; i++) x[i] = s[i / 16][i % 16];
-            if (SHAPED) {
-                if (capped) {
-#pragma unroll
-                    for (int i = 0; i < 32; i++) x[i] = cap2 * tanh_of(x[i] * scale2);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; i++) x[i] *= scale2;
-                }
-                if (bias) {
-                    const float pf = (float)(w.pos - j0 - 4 * hi);
-#pragma unroll
-                    for (int i = 0; i < 32; i++) {
-                        const int c = 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4;      // key j0 + 4 hi + c
-                        x[i] -= slope2 * fabsf(pf - (float)c);
-                    }
-                }
-            }
+            if (SHAPED) shape.apply(x, w.pos - j0 - 4 * hi);
             if (!w.whole(t)) {
 #pragma unroll
                 for (int i = 0; i < 32; i++)
@@ -449,27 +462,209 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
             nothing ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-// Joins the parts of a row: 8 rows a workgroup, 32 lanes a row, 4 columns each.
+// Few rows (at most 32 of a key head: new tokens over a cache): what bounds it
+// is reading the keys and values once.  Eight wavefronts have the same rows
+// and take tiles of 32 keys in turn, each at its own pace: keys go from memory
+// straight into the matrix operand, values through a piece of LDS that is the
+// wavefront's own (no barrier), and the next tile's loads are under way before
+// the softmax of this one.  At the end the eight sums are joined in LDS.
+constexpr int FEW_WAVES = 8, FEW_KEYS = 32;
+
+template <typename T, int NB, bool SHAPED>
+__global__ void __launch_bounds__(512, 2) few_rows_kernel(AttnArgs a)
+{
+    using L = Tile<NB>;
+    constexpr int SIZE = FEW_KEYS * L::PITCH, N = FEW_KEYS * L::CHUNKS / WAVE, STEP = WAVE / L::CHUNKS;
+    constexpr int SUMS = FEW_WAVES * FEW_ROWS * 32 * NB;
+    // values' tiles (16-bit) during the walk, sums (32-bit) afterwards
+    __shared__ __align__(16) char lds[SUMS * 4 > FEW_WAVES * SIZE * 2 ? SUMS * 4 : FEW_WAVES * SIZE * 2];
+    __shared__ float2 stats[FEW_WAVES][FEW_ROWS];
+    __shared__ int range[4];
+
+    const int units = a.batch * a.k_heads;
+    int id = spread(blockIdx.x, gridDim.x);
+    const int split = id % a.splits;
+    id /= a.splits;
+    const int lane = threadIdx.x % WAVE, hi = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const RowBlock<FEW_ROWS, FEW_WAVES * WAVE> w(a, id, 0, lane % 32, range);
+    const Unit &u = w.u;
+
+    // tiles of 32 keys, a multiple of eight for each part
+    int t0 = 2 * w.t0, t1 = min(2 * w.t1, (w.wave_end + FEW_KEYS - 1) / FEW_KEYS);
+    if (a.splits > 1) {
+        const int n = max(t1 - t0, 0), per = ((n + a.splits - 1) / a.splits + FEW_WAVES - 1) / FEW_WAVES * FEW_WAVES;
+        t0 = min(t0, max(t1, 0)) + per * split;
+        t1 = min(t0 + per, t1);
+    }
+
+    s16x8 q[2 * NB];
+    {
+        const char *qp = head_base(a.q, u.b, w.head) + w.query * a.q.position * 2;
+#pragma unroll
+        for (int s = 0; s < 2 * NB; s++) {
+            const int d = 16 * s + 8 * hi;
+            q[s] = d < a.head_dim ? *(const s16x8 *)(qp + d * 2) : s16x8{};
+        }
+    }
+    const Shape shape(a, w.head);
+    f32x16 o[NB] = {};
+    float m = LOWEST, l = 0;
+    const char *kb = head_base(a.k, u.b, u.g), *vb = head_base(a.v, u.b, u.g);
+    short *vt = (short *)lds + wave * SIZE;
+    const uint32_t koff = (uint32_t)(lane % 32 * (uint32_t)a.k.position + 8 * hi) * 2u;
+    const int vrow = lane / L::CHUNKS, vchunk = lane % L::CHUNKS;
+    const uint32_t voff = (uint32_t)(vrow * (uint32_t)a.v.position + vchunk * 8) * 2u;
+
+    s16x8 kf[2 * NB];
+    uint4 vr[N];
+    auto load = [&](int t) {
+        const int j0 = t * FEW_KEYS;
+        const char *kp = kb + j0 * a.k.position * 2, *vp = vb + j0 * a.v.position * 2;
+        const bool inside = j0 + FEW_KEYS <= u.len;
+        const bool in = inside || j0 + lane % 32 < u.len;
+#pragma unroll
+        for (int s = 0; s < 2 * NB; s++) {
+            if (s * 16 + 16 <= a.head_dim ? in : in && 16 * s + 8 * hi < a.head_dim) kf[s] = *(const s16x8 *)(kp + koff + s * 32);
+            else kf[s] = s16x8{};
+        }
+#pragma unroll
+        for (int n = 0; n < N; n++) {
+            if (vchunk * 8 < a.head_dim && (inside || j0 + vrow + n * STEP < u.len))
+                vr[n] = *(const uint4 *)(vp + n * STEP * a.v.position * 2 + voff);
+            else vr[n] = make_uint4(0, 0, 0, 0);
+        }
+    };
+    auto next = [&](int t) {
+        if (u.docs)
+            while (t < t1 && !w.near(t / 2)) t += FEW_WAVES;
+        return t;
+    };
+    int t = next(t0 + wave);
+    if (t < t1) load(t);
+    while (t < t1) {
+        const int j0 = t * FEW_KEYS, t2 = next(t + FEW_WAVES);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int n = 0; n < N; n++) *(uint4 *)(vt + L::at(vrow + n * STEP, vchunk)) = vr[n];
+        f32x16 s = {};
+#pragma unroll
+        for (int st = 0; st < 2 * NB; st++) s = T::mfma(kf[st], q[st], s);
+        if (t2 < t1) load(t2);
+        float x[16];
+        const float gain = SHAPED ? 1.0f : shape.scale2;
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[i] = s[i];
+        if (SHAPED) shape.apply(x, w.pos - j0 - 4 * hi);
+        if (j0 + FEW_KEYS > w.sure || u.docs) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) x[i] = w.sees(a, j0 + 4 * hi + 8 * (i / 4) + i % 4) ? x[i] : -INFINITY;
+        }
+        float most = x[0];
+#pragma unroll
+        for (int i = 1; i < 16; i++) most = fmaxf(most, x[i]);
+        most = fmaxf(most, other_half(most)) * gain;
+        if (__any(most > m + 8.0f)) {                    // as in the forward kernel above
+            const float m_new = fmaxf(m, most), f = exp2_(m - m_new);
+            m = m_new;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < NB; d++) o[d] *= f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            x[i] = exp2_(fmaf(x[i], gain, -m));
+            l += x[i];
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int kc = 0; kc < 2; kc++) {
+            const s16x8 p = rounded<T>(x + 8 * kc);
+#pragma unroll
+            for (int d = 0; d < NB; d++) o[d] = T::mfma(L::column_operand(vt, 16 * kc, d), p, o[d]);
+        }
+        t = t2;
+    }
+    l += other_half(l);
+
+    // the wavefronts' sums: row r, columns 4 c .. of wavefront v at ((v rows + r) COLS + c), four columns each
+    constexpr int COLS = 8 * NB;
+    const int rows = min(a.rows, FEW_ROWS);
+    __syncthreads();
+    f32x4 *sums = (f32x4 *)lds;
+    if (lane % 32 < rows) {
+#pragma unroll
+        for (int d = 0; d < NB; d++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                sums[(wave * rows + lane % 32) * COLS + 8 * d + 2 * e + hi] =
+                    f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+        if (hi == 0) stats[wave][lane] = make_float2(m, l);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * COLS; i += FEW_WAVES * WAVE) {
+        const int r = i / COLS, col = i % COLS * 4;
+        float most = LOWEST, total = 0;
+#pragma unroll
+        for (int v = 0; v < FEW_WAVES; v++) most = fmaxf(most, stats[v][r].x);
+        f32x4 sum = {};
+#pragma unroll
+        for (int v = 0; v < FEW_WAVES; v++) {
+            const float f = exp2_(stats[v][r].x - most);
+            total += stats[v][r].y * f;
+            sum += sums[v * rows * COLS + i] * f;
+        }
+        if (a.splits > 1) {
+            const int64_t at = ((int64_t)split * units + id) * a.rows + r;
+            if (col < a.head_dim) *(f32x4 *)(a.part_out + at * a.head_dim + col) = sum;
+            if (col == 0) a.part_stat[at] = make_float2(most, total);
+        } else {
+            const int query = r / a.group, head = u.g * a.group + r % a.group;
+            const bool nothing = total == 0;
+            if (col < a.head_dim) write_out<T>(a, u.b, head, query, col, nothing ? f32x4{} : sum * (1.0f / total));
+            if (a.lse && col == 0)
+                a.lse[((int64_t)u.b * a.k_heads * a.group + head) * a.q_len + query] =
+                    nothing ? -INFINITY : (most + __builtin_amdgcn_logf(total)) * LN2;
+        }
+    }
+}
+
+// Joins the parts (at most 256) of a row: a workgroup a row, eight groups of
+// 32 lanes take parts in turn, four columns a lane.
 template <typename T>
 __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
 {
-    const int64_t units = (int64_t)a.batch * a.k_heads, n = units * a.rows;
-    const int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
-    if (r >= n) return;
-    const int c = threadIdx.x % 32 * 4;
-    float m = LOWEST, l = 0;
-    for (int s = 0; s < a.splits; s++) m = fmaxf(m, a.part_stat[s * n + r].x);
+    __shared__ float factor[256];
+    __shared__ float2 waves[4];
+    __shared__ f32x4 sums[8][32];
+    const int64_t n = (int64_t)a.batch * a.k_heads * a.rows, r = blockIdx.x;
+    const int tid = threadIdx.x, g = tid / 32, c = tid % 32 * 4;
+    const float2 st = tid < a.splits ? a.part_stat[tid * n + r] : make_float2(LOWEST, 0.0f);
+    float m = st.x;
+#pragma unroll
+    for (int d = 1; d < WAVE; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    if (tid % WAVE == 0) waves[tid / WAVE].x = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(waves[0].x, waves[1].x), fmaxf(waves[2].x, waves[3].x));
+    const float f = exp2_(st.x - m);
+    factor[tid] = f;
+    float l = st.y * f;
+#pragma unroll
+    for (int d = 1; d < WAVE; d *= 2) l += __shfl_xor(l, d);
+    if (tid % WAVE == 0) waves[tid / WAVE].y = l;
+    __syncthreads();
+    l = (waves[0].y + waves[1].y) + (waves[2].y + waves[3].y);
     f32x4 o = {};
-    for (int s = 0; s < a.splits; s++) {
-        const float2 st = a.part_stat[s * n + r];
-        const float f = exp2_(st.x - m);
-        l += st.y * f;
-        if (c < a.head_dim) o += *(const f32x4 *)(a.part_out + (s * n + r) * a.head_dim + c) * f;
-    }
+    if (c < a.head_dim)
+        for (int s = g; s < a.splits; s += 8) o += *(const f32x4 *)(a.part_out + (s * n + r) * a.head_dim + c) * factor[s];
+    sums[g][tid % 32] = o;
+    __syncthreads();
+    if (g) return;
+#pragma unroll
+    for (int i = 1; i < 8; i++) o += sums[i][tid];
     const bool nothing = l == 0;
     const int64_t unit = r / a.rows;
-    const int row = (int)(r % a.rows), b = (int)(unit / a.k_heads), g = (int)(unit % a.k_heads);
-    const int query = row / a.group, head = g * a.group + row % a.group;
+    const int row = (int)(r % a.rows), b = (int)(unit / a.k_heads), kg = (int)(unit % a.k_heads);
+    const int query = row / a.group, head = kg * a.group + row % a.group;
     if (c < a.head_dim) write_out<T>(a, b, head, query, c, nothing ? f32x4{} : o * (1.0f / l));
     if (a.lse && c == 0)
         a.lse[((int64_t)b * a.k_heads * a.group + head) * a.q_len + query] =
@@ -525,7 +720,8 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 
     const int row_tiles = (a.rows + ROW_TILE - 1) / ROW_TILE;
     const int id = spread(blockIdx.x, gridDim.x);
-    const RowBlock w(a, id / row_tiles, (row_tiles - 1 - id % row_tiles) * ROW_TILE, range);
+    const int tile_row = (row_tiles - 1 - id % row_tiles) * ROW_TILE;
+    const RowBlock<ROW_TILE, 256> w(a, id / row_tiles, tile_row, tile_row + threadIdx.x / WAVE * 32 + threadIdx.x % 32, range);
     const Unit &u = w.u;
     const int lane = threadIdx.x % WAVE, hi = lane / 32;
 
@@ -851,11 +1047,13 @@ hipError_t doc_tiles(const AttnArgs &a, hipStream_t st)
 template <typename T, int NB, bool SHAPED> hipError_t forward_sized(const AttnArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
-    const unsigned n = (unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE) * a.splits);
-    forward_kernel<T, NB, SHAPED><<<n, 256, 0, st>>>(a);
+    if (a.rows <= FEW_ROWS)
+        few_rows_kernel<T, NB, SHAPED><<<(unsigned)(units * a.splits), FEW_WAVES * WAVE, 0, st>>>(a);
+    else
+        forward_kernel<T, NB, SHAPED><<<(unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE) * a.splits), 256, 0, st>>>(a);
     if (a.splits > 1) {
         if (hipError_t e = hipGetLastError()) return e;
-        join_kernel<T><<<(unsigned)((units * a.rows + 7) / 8), 256, 0, st>>>(a);
+        join_kernel<T><<<(unsigned)(units * a.rows), 256, 0, st>>>(a);
     }
     return hipGetLastError();
 }

@@ -69,12 +69,16 @@ struct Plan {
 
 // Parts that the keys are split into.  One part per row tile leaves most of
 // the 256 compute units idle where there are few rows; each part costs a
-// partial result (32-bit, written and read again) and the join's launch.
-int32_t splits_for(int64_t tiles, int64_t key_tiles)
+// partial result (32-bit, written and read again) and the join's launch.  With
+// few rows a part has 512 keys at least (two tiles for each of its eight
+// wavefronts), otherwise 256.
+int32_t splits_for(int64_t units, int64_t rows, int64_t k_len)
 {
-    if (tiles >= 256 || key_tiles < 8) return 1;
-    const int64_t want = (512 + tiles - 1) / tiles;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(want, key_tiles / 4), 256));
+    const bool few = rows <= FEW_ROWS;
+    const int64_t groups = few ? units : units * ((rows + ROW_TILE - 1) / ROW_TILE);
+    if (groups >= (few ? 1024 : 256)) return 1;
+    const int64_t want = ((few ? 1024 : 512) + groups - 1) / std::max<int64_t>(groups, 1);
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(want, k_len / (few ? 512 : 256)), 256));
 }
 
 // Parts that the rows are cut into for dK and dV.  A key block's work ranges
@@ -92,7 +96,7 @@ Plan make_plan(const dtr_attn *a, bool backward)
     Plan p{};
     const int64_t group = a->q_heads / a->k_heads, rows = a->q_len * group;
     const int64_t units = (int64_t)a->batch * a->k_heads, key_tiles = (a->k_len + KEY_TILE - 1) / KEY_TILE;
-    p.splits = backward ? 1 : splits_for(units * ((rows + ROW_TILE - 1) / ROW_TILE), key_tiles);
+    p.splits = backward ? 1 : splits_for(units, rows, a->k_len);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
