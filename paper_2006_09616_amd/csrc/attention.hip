@@ -463,15 +463,17 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
 }
 
 // Few rows (at most 32 of a key head: new tokens over a cache): what bounds it
-// is reading the keys and values once.  Eight wavefronts have the same rows
+// is reading the keys and values once.  Four wavefronts have the same rows
 // and take tiles of 32 keys in turn, each at its own pace: keys go from memory
 // straight into the matrix operand, values through a piece of LDS that is the
 // wavefront's own (no barrier), and the next tile's loads are under way before
-// the softmax of this one.  At the end the eight sums are joined in LDS.
-constexpr int FEW_WAVES = 8, FEW_KEYS = 32;
+// the softmax of this one.  At the end the four sums are joined in LDS.  Two
+// workgroups of four share a compute unit (one of eight measured 47 against 39
+// us on 12 key heads of 30011 keys: nothing runs beside its start and end).
+constexpr int FEW_WAVES = 4, FEW_KEYS = 32;
 
 template <typename T, int NB, bool SHAPED>
-__global__ void __launch_bounds__(512, 2) few_rows_kernel(AttnArgs a)
+__global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
     constexpr int SIZE = FEW_KEYS * L::PITCH, N = FEW_KEYS * L::CHUNKS / WAVE, STEP = WAVE / L::CHUNKS;
@@ -489,7 +491,7 @@ __global__ void __launch_bounds__(512, 2) few_rows_kernel(AttnArgs a)
     const RowBlock<FEW_ROWS, FEW_WAVES * WAVE> w(a, id, 0, lane % 32, range);
     const Unit &u = w.u;
 
-    // tiles of 32 keys, a multiple of eight for each part
+    // tiles of 32 keys, a multiple of FEW_WAVES for each part
     int t0 = 2 * w.t0, t1 = min(2 * w.t1, (w.wave_end + FEW_KEYS - 1) / FEW_KEYS);
     if (a.splits > 1) {
         const int n = max(t1 - t0, 0), per = ((n + a.splits - 1) / a.splits + FEW_WAVES - 1) / FEW_WAVES * FEW_WAVES;
@@ -1079,6 +1081,7 @@ template <typename T> hipError_t forward_typed(const AttnArgs &a, hipStream_t st
 {
     const bool shaped = a.cap > 0 || a.slopes;
     if (a.head_dim <= 64) return shaped ? forward_sized<T, 2, true>(a, st) : forward_sized<T, 2, false>(a, st);
+    if (a.head_dim <= 96) return shaped ? forward_sized<T, 3, true>(a, st) : forward_sized<T, 3, false>(a, st);
     return shaped ? forward_sized<T, 4, true>(a, st) : forward_sized<T, 4, false>(a, st);
 }
 
@@ -1086,6 +1089,7 @@ template <typename T> hipError_t backward_typed(const AttnArgs &a, hipStream_t s
 {
     const bool shaped = a.cap > 0 || a.slopes;
     if (a.head_dim <= 64) return shaped ? backward_sized<T, 2, true>(a, st) : backward_sized<T, 2, false>(a, st);
+    if (a.head_dim <= 96) return shaped ? backward_sized<T, 3, true>(a, st) : backward_sized<T, 3, false>(a, st);
     return shaped ? backward_sized<T, 4, true>(a, st) : backward_sized<T, 4, false>(a, st);
 }
 

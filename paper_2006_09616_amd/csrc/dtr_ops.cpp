@@ -69,15 +69,18 @@ struct Plan {
 
 // Parts that the keys are split into.  One part per row tile leaves most of
 // the 256 compute units idle where there are few rows; each part costs a
-// partial result (32-bit, written and read again) and the join's launch.  With
-// few rows a part has 512 keys at least (two tiles for each of its eight
-// wavefronts), otherwise 256.
+// partial result (32-bit, written and read again) and the join's launch.
+//   Few rows: two workgroups are resident on each compute unit.  Up to 128
+// units, parts for one round of them (12 units of 30011 keys: 33 us with 504
+// workgroups, 39 with 696); beyond, where lengths are many and unequal, for
+// two (256 units of 8192 to 16384 keys: 287 us with 1024, 319 with 512).  A
+// part has 512 keys at least.
+//   Others: parts for two rounds of one workgroup, 256 keys at least.
 int32_t splits_for(int64_t units, int64_t rows, int64_t k_len)
 {
     const bool few = rows <= FEW_ROWS;
-    const int64_t groups = few ? units : units * ((rows + ROW_TILE - 1) / ROW_TILE);
-    if (groups >= (few ? 1024 : 256)) return 1;
-    const int64_t want = ((few ? 1024 : 512) + groups - 1) / std::max<int64_t>(groups, 1);
+    const int64_t groups = std::max<int64_t>(few ? units : units * ((rows + ROW_TILE - 1) / ROW_TILE), 1);
+    const int64_t want = few ? (groups <= 128 ? 512 : 1024) / groups : groups >= 256 ? 1 : (512 + groups - 1) / groups;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(want, k_len / (few ? 512 : 256)), 256));
 }
 
@@ -184,11 +187,12 @@ int check_logprobs(int32_t type, int64_t rows, int64_t vocab, int32_t top)
 }
 
 // Parts of a row read by workgroups of their own: one workgroup a row leaves
-// the card idle where there are few rows.  A part has at least 4096 columns.
+// the card idle where there are few rows.  A part has at least 4096 columns,
+// and a row 64 parts at most.
 int32_t logprob_splits(int64_t rows, int64_t vocab)
 {
     if (rows >= 256 || vocab < 8192) return 1;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>((512 + rows - 1) / rows, vocab / 4096));
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((512 + rows - 1) / rows, 64), vocab / 4096));
 }
 
 }  // namespace
@@ -302,7 +306,7 @@ int dtr_logprobs_workspace_bytes(int32_t type, int64_t rows, int64_t vocab, int3
     if (!bytes) return fail(DTR_EINVAL, "null bytes");
     if (int rc = check_logprobs(type, rows, vocab, top)) return rc;
     const int32_t s = logprob_splits(rows, vocab);
-    *bytes = s > 1 ? align_up(sizeof(float) * 4 * rows * s * SEGS) + align_up(sizeof(float2) * rows * s * SEGS * top) : 0;
+    *bytes = s > 1 ? align_up(sizeof(float) * 4 * rows * s) + align_up(sizeof(float2) * rows * s * top) : 0;
     return DTR_OK;
 }
 
@@ -333,7 +337,7 @@ int dtr_logprobs_forward(int32_t type, int64_t rows, int64_t vocab, int32_t top,
     a.top_logp = top_logp;
     a.top_ids = top_ids;
     a.part = (float *)workspace;
-    a.part_top = (float2 *)((char *)workspace + align_up(sizeof(float) * 4 * rows * a.splits * SEGS));
+    a.part_top = (float2 *)((char *)workspace + align_up(sizeof(float) * 4 * rows * a.splits));
     return launched(launch_logprobs(a, type, (hipStream_t)stream), "log probabilities");
 }
 

@@ -46,8 +46,8 @@ struct LogpArgs {
     const int64_t *tokens;
     float *logp, *entropy, *lse, *top_logp;
     int64_t *top_ids;
-    float *part;                  // [rows][segments][4] maximum, sum, weighted sum, entries
-    float2 *part_top;             // [rows][segments][top] value, column (as bits)
+    float *part;                  // [rows][splits][4] maximum, sum, weighted sum
+    float2 *part_top;             // [rows][splits][top] value, column (as bits)
 };
 
 struct LogpGradArgs {

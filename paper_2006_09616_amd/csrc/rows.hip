@@ -107,20 +107,22 @@ template <typename T> hipError_t dropout_typed(const DropArgs &a, hipStream_t st
 
 // ---- log probabilities -------------------------------------------------------
 // One pass: a running maximum m, l = sum exp(x - m) and w = sum exp(x - m)
-// (x - m) give lse = m + log l and entropy = log l - w / l.  The alternatives
-// are kept by each wavefront as a list sorted over its lanes; an element is
-// compared with the list's last only, through the maximum of its vector.
+// (x - m) give lse = m + log l and entropy = log l - w / l (w and log l
+// in units of log 2, as the exponential instruction has it).
 
 constexpr float LOWEST = -3.402823466e+38f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
+// m: maximum; l = sum exp(x - m); w = sum exp(x - m) (x - m) log2(e).  The
+// maximum is subtracted before the factor log2(e): that times the type's
+// lowest value would be minus infinity.
 struct Stat { float m, l, w; };
 
 __device__ __forceinline__ Stat join(Stat a, Stat b)
 {
     const float m = fmaxf(a.m, b.m);
-    const float da = fmaxf(a.m - m, -1e4f), db = fmaxf(b.m - m, -1e4f);
-    const float ea = __builtin_amdgcn_exp2f(da * LOG2E), eb = __builtin_amdgcn_exp2f(db * LOG2E);
+    const float da = fmaxf((a.m - m) * LOG2E, -1e4f), db = fmaxf((b.m - m) * LOG2E, -1e4f);
+    const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
     return {m, a.l * ea + b.l * eb, (a.w + da * a.l) * ea + (b.w + db * b.l) * eb};
 }
 
@@ -134,248 +136,440 @@ __device__ __forceinline__ Stat join_wave(Stat s)
     return s;
 }
 
-// The wavefront's list: lane i < count holds the i-th largest value and its
-// column.  Elements come in ascending order of columns, so among equals the
-// one that came first stays in front.
+// Lane exchanges within the vector unit: they cost what an addition costs,
+// where one through LDS would wait a hundred cycles.
+template <int CONTROL> __device__ __forceinline__ float moved(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CONTROL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float lane_value(float v, int lane)              // lane: uniform
+{
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+__device__ __forceinline__ float wave_max(float v)                          // uniform
+{
+    v = fmaxf(v, moved<0x111>(v));                                          // row_shr:1 .. 8: rows of 16 lanes
+    v = fmaxf(v, moved<0x112>(v));
+    v = fmaxf(v, moved<0x114>(v));
+    v = fmaxf(v, moved<0x118>(v));
+    v = fmaxf(v, moved<0x142>(v));                                          // row_bcast:15, row_bcast:31
+    v = fmaxf(v, moved<0x143>(v));
+    return lane_value(v, WAVE - 1);
+}
+
+// A wavefront's list of alternatives, which takes elements in any number and
+// order: an element is compared with the list's last, through the maximum of
+// its vector.  Lane i < count holds the i-th largest value and its
+// column, the lower column first among equals.
 struct Top {
     float value;
     int32_t column;
-    int count;                    // uniform
-    float last;                   // uniform: the k-th value once the list is full
+    int count;                    // uniform, as all below
+    float last;                   // the k-th value once the list is full
+    int32_t last_column;
+    float floor;                  // until then: k elements or more are at least this
 
     __device__ void clear()
     {
         value = 0;
         column = -1;
         count = 0;
-        last = LOWEST;
+        last = floor = -INFINITY;
+        last_column = -1;
     }
 
-    __device__ bool wants(float v, int k) const { return count < k || v > last; }
+    // whether an element of a later column than all in the list may enter it
+    __device__ bool wants(float v, int k) const { return count < k ? v >= floor : v > last; }
 
-    __device__ void insert(float v, int32_t c, int k)      // uniform arguments
+    __device__ void offer(float v, int32_t c, int k)       // uniform arguments, any column
     {
+        if (count == k && !(v > last || (v == last && c < last_column))) return;
         const int lane = threadIdx.x % WAVE;
-        const uint64_t ahead = __ballot(lane < count && value >= v);
-        const int at = __popcll(ahead);
-        const float pv = __shfl_up(value, 1);
-        const int32_t pc = __shfl_up(column, 1);
-        if (lane > at) {
-            value = pv;
-            column = pc;
-        }
-        if (lane == at) {
-            value = v;
-            column = c;
-        }
+        const int at = __popcll(__ballot(lane < count && (value > v || (value == v && column < c))));
+        const float pv = moved<0x138>(value);                               // wave_shr:1
+        const int32_t pc = __builtin_amdgcn_update_dpp(column, column, 0x138, 0xf, 0xf, false);
+        value = lane > at ? pv : lane == at ? v : value;
+        column = lane > at ? pc : lane == at ? c : column;
         if (count < k) count++;
         if (lane >= count) column = -1;
-        if (count == k) last = __shfl(value, k - 1);
+        if (count == k) {
+            last = lane_value(value, k - 1);
+            last_column = __builtin_amdgcn_readlane(column, k - 1);
+        }
+    }
+
+    // The k-th largest of 64 lanes' values bounds the k-th largest of all from
+    // below.  With the maxima of the first 2048 elements, 24 of them enter a
+    // list of 20 where 112 would enter one that grows from nothing.
+    __device__ void set_floor(float v, int k)
+    {
+        const int lane = threadIdx.x % WAVE;
+        v = v == v ? v : -INFINITY;
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < WAVE; j++) {
+            const float o = lane_value(v, j);
+            rank += o > v || (o == v && j < lane);
+        }
+        floor = lane_value(v, __ffsll(__ballot(rank == k - 1)) - 1);
     }
 };
 
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int d = 1; d < WAVE; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
-}
-
-// Candidates of one step, N a lane, columns ascending over lane and element.
+// Candidates of one step, N a lane, all of later columns than the list's.
 template <int N>
-__device__ void top_step(Top &top, const float (&x)[N], uint32_t open, int32_t column0, int k)
+__device__ void top_step(Top &top, const float (&x)[N], bool in, int32_t column0, int k)
 {
-    while (true) {
-        float best = -INFINITY;
-        int at = -1;
+    const bool full = top.count == k;
+    const float bar = full ? top.last : top.floor;
 #pragma unroll
-        for (int e = 0; e < N; e++) {
-            const float v = x[e] == x[e] ? x[e] : -INFINITY;        // a NaN counts as the least
-            if ((open >> e & 1) && (at < 0 || v > best)) {
-                best = v;
-                at = e;
-            }
+    for (int e = 0; e < N; e++) {
+        const float v = x[e] == x[e] ? x[e] : -INFINITY;            // a NaN counts as the least
+        for (uint64_t open = __ballot(in && (full ? v > bar : v >= bar)); open; open &= open - 1) {
+            const int lane = __ffsll((unsigned long long)open) - 1;
+            top.offer(lane_value(v, lane), __builtin_amdgcn_readlane(column0, lane) + e, k);
         }
-        const bool any = at >= 0 && top.wants(best, k);
-        if (!__ballot(any)) return;
-        const float most = wave_max(any ? best : -INFINITY);
-        const int lane = __ffsll(__ballot(any && best == most)) - 1;
-        top.insert(most, __shfl(column0 + at, lane), k);
-        if ((int)(threadIdx.x % WAVE) == lane) open &= ~(1u << at);
     }
 }
 
+// Returns the largest of the x.
 template <int N>
-__device__ __forceinline__ void stat_step(Stat &s, const float (&x)[N])
+__device__ __forceinline__ float stat_step(Stat &s, const float (&x)[N])
 {
     float most = x[0];
 #pragma unroll
     for (int e = 1; e < N; e++) most = fmaxf(most, x[e]);
     if (most > s.m) {
-        const float d = fmaxf(s.m - most, -1e4f), f = __builtin_amdgcn_exp2f(d * LOG2E);
+        const float d = fmaxf((s.m - most) * LOG2E, -1e4f), f = __builtin_amdgcn_exp2f(d);
         s.w = (s.w + d * s.l) * f;
         s.l *= f;
         s.m = most;
     }
 #pragma unroll
     for (int e = 0; e < N; e++) {
-        const float d = x[e] - s.m;
-        const float p = __builtin_amdgcn_exp2f(d * LOG2E);
+        const float d = (x[e] - s.m) * LOG2E;
+        const float p = __builtin_amdgcn_exp2f(d);
         s.l += p;                                                  // carries a NaN
-        s.w += p * fmaxf(d, -1e4f);                                // 0 for minus infinity
+        s.w = fmaf(p, fmaxf(d, -1e4f), s.w);                       // 0 for minus infinity
     }
+    return most;
 }
 
-// What a wavefront's segment or a whole row comes to: written for a join, or
-// as the row's results.
-__device__ void finish_row(const LogpArgs &a, int64_t row, Stat s, const Top &top, float token_logit, int64_t token)
+// A row's results; lane i < top holds the i-th alternative.
+__device__ void finish_row(const LogpArgs &a, int64_t row, Stat s, float value, int32_t column, float token_logit, int64_t token)
 {
     const int lane = threadIdx.x % WAVE;
     const bool nothing = s.l == 0;                                  // minus infinity throughout
-    const float log_l = __builtin_amdgcn_logf(s.l) * LN2;
-    const float lse = nothing ? -INFINITY : s.m + log_l;
+    const float log_l = __builtin_amdgcn_logf(s.l);
+    const float lse = nothing ? -INFINITY : s.m + log_l * LN2;
     if (lane == 0) {
         a.lse[row] = lse;
-        a.entropy[row] = nothing ? 0.0f : log_l - s.w / s.l;
+        a.entropy[row] = nothing ? 0.0f : (log_l - s.w / s.l) * LN2;
         a.logp[row] = token < 0 ? 0.0f : token >= a.vocab ? NAN : nothing ? -INFINITY : token_logit - lse;
     }
     if (lane < a.top) {
-        a.top_logp[row * a.top + lane] = nothing ? -INFINITY : top.value - lse;
-        a.top_ids[row * a.top + lane] = top.column < 0 ? 0 : top.column;
+        a.top_logp[row * a.top + lane] = nothing ? -INFINITY : value - lse;
+        a.top_ids[row * a.top + lane] = column < 0 ? 0 : column;
     }
 }
 
-// a list entry of every lane with column >= 0, lists in ascending order of columns
+// a list entry of every lane with column >= 0
 __device__ void join_list(Top &top, float v, int32_t c, int k)
 {
-    bool open = c >= 0;
-    while (true) {
-        const bool any = open && top.wants(v, k);
-        if (!__ballot(any)) return;
-        const float most = wave_max(any ? v : -INFINITY);
-        const int lane = __ffsll(__ballot(any && v == most)) - 1;
-        top.insert(most, __shfl(c, lane), k);
-        if ((int)(threadIdx.x % WAVE) == lane) open = false;
+    for (uint64_t open = __ballot(c >= 0); open; open &= open - 1) {
+        const int lane = __ffsll((unsigned long long)open) - 1;
+        top.offer(lane_value(v, lane), __builtin_amdgcn_readlane(c, lane), k);
     }
 }
 
-// GROUP wavefronts read a row (one, or SEGS), each a contiguous segment.
-template <typename T, int GROUP, bool TOP>
-__global__ void __launch_bounds__(256) logprob_kernel(LogpArgs a)
+constexpr int AHEAD = 4;
+
+// A wavefront's part of a row: whole 16-byte vectors v0 .. v1 - 1 of those
+// from `head` on, and elements before (at the row's start) and after them (at
+// its end), fewer than a vector's.
+template <typename T> struct Segment {
+    using R = typename T::raw;
+    static constexpr int N = T::vec;
+    const R *x;
+    int head, v0, v1, tail0, tails;      // columns 0 .. head - 1 if first, tail0 .. tail0 + tails - 1 if last
+    bool first;
+
+    __device__ Segment(const R *row, int vocab, int seg, int segs) : x(row)
+    {
+        const int mis = (int)((uintptr_t)row % 16 / sizeof(R));
+        head = min(mis ? N - mis : 0, vocab);
+        const int vecs = (vocab - head) / N, per = (vecs + segs - 1) / segs;
+        v0 = min(per * seg, vecs);
+        v1 = min(v0 + per, vecs);
+        first = seg == 0;
+        tail0 = head + vecs * N;
+        tails = seg == segs - 1 ? vocab - tail0 : 0;
+    }
+    __device__ Pack<R, N> vector(int v) const { return *(const Pack<R, N> *)(x + head + (int64_t)v * N); }
+};
+
+template <typename T>
+__device__ __forceinline__ Stat segment_stat(const Segment<T> &g)
 {
     using R = typename T::raw;
     constexpr int N = T::vec;
-    __shared__ float part[SEGS][3];
-    __shared__ float2 lists[SEGS][32];
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
-    const int64_t unit = GROUP == 1 ? (int64_t)blockIdx.x * SEGS + wave : blockIdx.x;
-    const int64_t row = GROUP == 1 ? unit : unit / a.splits;
-    if (GROUP == 1 && row >= a.rows) return;
-    const int segs = GROUP == 1 ? 1 : a.splits * SEGS;
-    const int seg = GROUP == 1 ? 0 : (int)(unit % a.splits) * SEGS + wave;
-    const R *x = (const R *)a.x + row * a.stride;
-
-    // head up to the first 16-byte boundary, whole vectors, tail
-    const int64_t mis = (uintptr_t)x % 16 / sizeof(R);
-    const int64_t head = min(mis ? N - mis : (int64_t)0, a.vocab);
-    const int64_t vecs = (a.vocab - head) / N, tail0 = head + vecs * N;
-    const int64_t per = (vecs + segs - 1) / segs, v0 = min(per * seg, vecs), v1 = min(v0 + per, vecs);
-
+    const int lane = threadIdx.x % WAVE;
     Stat s = {LOWEST, 0, 0};
+    Pack<R, N> ahead[AHEAD];
+    auto load = [&](int v) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++)
+            if (v + i * WAVE + lane < g.v1) ahead[i] = g.vector(v + i * WAVE + lane);
+    };
+    load(g.v0);
+    for (int v = g.v0; v < g.v1; v += AHEAD * WAVE) {
+        float e[AHEAD][N];
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++) {
+            const bool in = v + i * WAVE + lane < g.v1;
+#pragma unroll
+            for (int j = 0; j < N; j++) e[i][j] = in ? (float)ahead[i].e[j] : -INFINITY;
+        }
+        load(v + AHEAD * WAVE);
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++) stat_step(s, e[i]);
+    }
+    if (g.first && lane < g.head) {
+        const float e[1] = {(float)g.x[lane]};
+        stat_step(s, e);
+    }
+    if (lane < g.tails) {
+        const float e[1] = {(float)g.x[g.tail0 + lane]};
+        stat_step(s, e);
+    }
+    return s;
+}
+
+// The alternatives of a wavefront's segment, by the list.
+template <typename T>
+__device__ Top segment_top(const Segment<T> &g, int k)
+{
+    constexpr int N = T::vec;
+    const int lane = threadIdx.x % WAVE;
     Top top;
     top.clear();
-    auto edge = [&](int64_t c0, int64_t n) {                        // fewer than N elements, one a lane
-        float e[1] = {lane < n ? (float)x[c0 + lane] : -INFINITY};
-        stat_step(s, e);
-        if (TOP) top_step(top, e, lane < n ? 1u : 0u, (int32_t)c0 + lane, a.top);
+    auto edge = [&](int c0, int n) {
+        const float e[1] = {lane < n ? (float)g.x[c0 + lane] : -INFINITY};
+        top_step(top, e, lane < n, c0 + lane, k);
     };
-    if (seg == 0 && head) edge(0, head);
-    for (int64_t v = v0; v < v1; v += WAVE) {
-        float e[N];
-        const bool in = v + lane < v1;
-        Pack<R, N> p;
-        if (in) p = *(const Pack<R, N> *)(x + head + (v + lane) * N);
+    if (g.first && g.head) edge(0, g.head);
+    for (int v = g.v0; v < g.v1; v += WAVE) {
+        const bool in = v + lane < g.v1;
+        float e[N], most = -INFINITY;
+        auto p = g.vector(in ? v + lane : v);
 #pragma unroll
-        for (int i = 0; i < N; i++) e[i] = in ? (float)p.e[i] : -INFINITY;
-        stat_step(s, e);
-        if (TOP) top_step(top, e, in ? (1u << N) - 1 : 0u, (int32_t)(head + (v + lane) * N), a.top);
+        for (int j = 0; j < N; j++) {
+            e[j] = in ? (float)p.e[j] : -INFINITY;
+            most = fmaxf(most, e[j]);
+        }
+        if (v == g.v0) top.set_floor(most, k);
+        if (__ballot(in && top.wants(most, k))) top_step(top, e, in, g.head + (v + lane) * N, k);
     }
-    if (seg == segs - 1 && tail0 < a.vocab) edge(tail0, a.vocab - tail0);
-    s = join_wave(s);
+    if (g.tails) edge(g.tail0, g.tails);
+    return top;
+}
 
+// A workgroup's alternatives among its part of a row.  The statistics' pass
+// has left each lane the maximum of its own columns: the k-th largest of these
+// 256 bounds the part's k-th largest element from below, and just the k lanes
+// that reach it (more where maxima are equal) own elements that do.  Their
+// columns are read again, and of the few elements found each counts how many
+// are ahead of it.  Where more are found than there is room for, as among many
+// equal ones, or fewer than k numbers, the wavefronts' lists do it instead.
+constexpr int FOUND = 512;
+
+struct TopScratch {
+    float most[256];
+    int lanes[256];
+    float2 found[FOUND];
+    float2 lists[SEGS][32];
+    float2 best[32];                     // the result: value, column (as bits; -1: none), largest first
+    int n_lanes, n_found;
+    float bar;
+};
+
+template <typename T>
+__device__ void part_top(TopScratch &w, const Segment<T> &g, const typename T::raw *x, int vocab, int seg0, int segs, float most, int k)
+{
+    constexpr int N = T::vec;
+    const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE;
+    w.most[tid] = most;
+    if (tid == 0) w.n_lanes = w.n_found = 0;
+    if (tid < 32) w.best[tid] = make_float2(0, __int_as_float(-1));
+    __syncthreads();
+    int rank = 0;
+    for (int j = 0; j < 256; j += 4) {
+        const float4 o = *(const float4 *)&w.most[j];
+        rank += (o.x > most || (o.x == most && j < tid)) + (o.y > most || (o.y == most && j + 1 < tid)) +
+                (o.z > most || (o.z == most && j + 2 < tid)) + (o.w > most || (o.w == most && j + 3 < tid));
+    }
+    if (rank == k - 1) w.bar = most;
+    __syncthreads();
+    const float bar = w.bar;
+    if (most >= bar) w.lanes[atomicAdd(&w.n_lanes, 1)] = tid;
+    auto offer = [&](float v, int c) {
+        if (!(v >= bar)) return;
+        const int at = atomicAdd(&w.n_found, 1);
+        if (at < FOUND) w.found[at] = make_float2(v, __int_as_float(c));
+    };
+    if (g.first && lane < g.head) offer((float)x[lane], lane);
+    if (lane < g.tails) offer((float)x[g.tail0 + lane], g.tail0 + lane);
+    __syncthreads();
+    // all lanes with equal maxima: as many lanes' columns as the row has
+    const int vecs = (vocab - g.head) / N, per = (vecs + segs - 1) / segs, each = (per + WAVE - 1) / WAVE;
+    const int n_lanes = w.n_lanes;
+    if (n_lanes <= 4 * k)
+        for (int i = tid; i < n_lanes * each; i += 256) {
+            const int owner = w.lanes[i / each];
+            const int begin = min(per * (seg0 + owner / WAVE), vecs), end = min(begin + per, vecs);
+            const int v = begin + owner % WAVE + i % each * WAVE;
+            if (v >= end) continue;
+            const auto p = g.vector(v);
+#pragma unroll
+            for (int e = 0; e < N; e++) offer((float)p.e[e], g.head + v * N + e);
+        }
+    __syncthreads();
+    const int n = w.n_found;
+    if (n_lanes <= 4 * k && n <= FOUND && n >= k) {
+        for (int i = tid; i < n; i += 256) {
+            const float2 mine = w.found[i];
+            int ahead = 0;
+            for (int j = 0; j < n; j++) {
+                const float2 o = w.found[j];
+                ahead += o.x > mine.x || (o.x == mine.x && __float_as_int(o.y) < __float_as_int(mine.y));
+            }
+            if (ahead < k) w.best[ahead] = mine;
+        }
+    } else {
+        Top top = segment_top<T>(g, k);
+        if (lane < k) w.lists[wave][lane] = make_float2(top.value, __int_as_float(top.column));
+        __syncthreads();
+        if (wave == 0) {
+            for (int i = 1; i < SEGS; i++) {
+                const float2 t = lane < k ? w.lists[i][lane] : make_float2(0, __int_as_float(-1));
+                join_list(top, t.x, __float_as_int(t.y), k);
+            }
+            if (lane < k) w.best[lane] = make_float2(top.value, __int_as_float(top.column));
+        }
+    }
+    __syncthreads();
+}
+
+// Short rows: a wavefront each.
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(256) logprob_short(LogpArgs a)
+{
+    using R = typename T::raw;
+    const int64_t row = (int64_t)blockIdx.x * SEGS + threadIdx.x / WAVE;
+    if (row >= a.rows) return;
+    const R *x = (const R *)a.x + row * a.stride;
     const int64_t token = a.tokens[row];
     const float logit = token >= 0 && token < a.vocab ? (float)x[token] : 0.0f;
-    if (GROUP == 1) {
-        finish_row(a, row, s, top, logit, token);
-        return;
-    }
-    if (a.splits > 1) {
-        float *o = a.part + (row * segs + seg) * 4;
-        if (lane == 0) {
-            o[0] = s.m;
-            o[1] = s.l;
-            o[2] = s.w;
-        }
-        if (TOP && lane < a.top)
-            a.part_top[(row * segs + seg) * a.top + lane] = make_float2(top.value, __int_as_float(top.column));
-        return;
-    }
+    const Segment<T> g(x, (int)a.vocab, 0, 1);
+    const Stat s = join_wave(segment_stat<T>(g));
+    Top top;
+    top.clear();
+    if (TOP) top = segment_top<T>(g, a.top);
+    finish_row(a, row, s, top.value, top.column, logit, token);
+}
+
+// A workgroup a row, or a part of one; a contiguous segment for each wavefront.
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(256) logprob_kernel(LogpArgs a)
+{
+    using R = typename T::raw;
+    __shared__ float part[SEGS][3];
+    __shared__ TopScratch scratch;
+    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    const int row = a.splits > 1 ? (int)blockIdx.x / a.splits : (int)blockIdx.x, split = (int)blockIdx.x - row * a.splits;
+    const R *x = (const R *)a.x + row * a.stride;
+    const int64_t token = a.tokens[row];
+    const float logit = token >= 0 && token < a.vocab ? (float)x[token] : 0.0f;
+    const int seg0 = split * SEGS, segs = a.splits * SEGS;
+    const Segment<T> g(x, (int)a.vocab, seg0 + __builtin_amdgcn_readfirstlane(wave), segs);
+    Stat s = segment_stat<T>(g);
+    const float most = s.m;
+    s = join_wave(s);
     if (lane == 0) {
         part[wave][0] = s.m;
         part[wave][1] = s.l;
         part[wave][2] = s.w;
     }
-    if (TOP && lane < a.top) lists[wave][lane] = make_float2(top.value, __int_as_float(top.column));
-    __syncthreads();
+    if (TOP) part_top<T>(scratch, g, x, (int)a.vocab, seg0, segs, most, a.top);
+    else __syncthreads();
     if (wave) return;
     s = {part[0][0], part[0][1], part[0][2]};
-    for (int g = 1; g < SEGS; g++) s = join(s, {part[g][0], part[g][1], part[g][2]});
-    if (TOP)
-        for (int g = 1; g < SEGS; g++) {
-            const float2 t = lane < a.top ? lists[g][lane] : make_float2(0, __int_as_float(-1));
-            join_list(top, t.x, __float_as_int(t.y), a.top);
-        }
-    finish_row(a, row, s, top, logit, token);
+    for (int i = 1; i < SEGS; i++) s = join(s, {part[i][0], part[i][1], part[i][2]});
+    const float2 best = TOP && lane < a.top ? scratch.best[lane] : make_float2(0, __int_as_float(-1));
+    if (a.splits == 1) {
+        finish_row(a, row, s, best.x, __float_as_int(best.y), logit, token);
+        return;
+    }
+    float *o = a.part + (int64_t)blockIdx.x * 4;
+    if (lane == 0) {
+        o[0] = s.m;
+        o[1] = s.l;
+        o[2] = s.w;
+    }
+    if (TOP && lane < a.top) a.part_top[(int64_t)blockIdx.x * a.top + lane] = best;
 }
 
-// the segments of a row that several workgroups read: one wavefront a row
+// The parts of a row that several workgroups read (at most 64): the
+// alternatives by counting how many of all parts' are ahead of each.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(64) logprob_join(LogpArgs a)
+__global__ void __launch_bounds__(256) logprob_join(LogpArgs a)
 {
     using R = typename T::raw;
-    const int lane = threadIdx.x;
+    __shared__ float2 all[64 * 32];
+    __shared__ float2 best[32];
+    const int tid = threadIdx.x, lane = tid % WAVE;
     const int64_t row = blockIdx.x;
-    const int segs = a.splits * SEGS;
-    Stat s = {LOWEST, 0, 0};
-    for (int g = lane; g < segs; g += WAVE) {
-        const float *o = a.part + (row * segs + g) * 4;
-        s = join(s, {o[0], o[1], o[2]});
-    }
-    s = join_wave(s);
-    Top top;
-    top.clear();
-    if (TOP)
-        for (int e0 = 0; e0 < segs * a.top; e0 += WAVE) {
-            const int e = e0 + lane;
-            const float2 t = e < segs * a.top ? a.part_top[row * segs * a.top + e] : make_float2(0, __int_as_float(-1));
-            join_list(top, t.x, __float_as_int(t.y), a.top);
-        }
     const int64_t token = a.tokens[row];
-    const R *x = (const R *)a.x + row * a.stride;
-    finish_row(a, row, s, top, token >= 0 && token < a.vocab ? (float)x[token] : 0.0f, token);
+    const float logit = token >= 0 && token < a.vocab ? (float)((const R *)a.x)[row * a.stride + token] : 0.0f;
+    Stat s = {LOWEST, 0, 0};
+    if (lane < a.splits) {
+        const float *o = a.part + (row * a.splits + lane) * 4;
+        s = {o[0], o[1], o[2]};
+    }
+    if (TOP) {
+        const int n = a.splits * a.top;
+        for (int i = tid; i < n; i += 256) all[i] = a.part_top[row * n + i];
+        if (tid < 32) best[tid] = make_float2(0, __int_as_float(-1));
+        __syncthreads();
+        for (int i = tid; i < n; i += 256) {
+            const float2 mine = all[i];
+            if (__float_as_int(mine.y) < 0) continue;
+            int ahead = 0;
+            for (int j = 0; j < n; j++) {
+                const float2 o = all[j];
+                ahead += __float_as_int(o.y) >= 0 &&
+                         (o.x > mine.x || (o.x == mine.x && __float_as_int(o.y) < __float_as_int(mine.y)));
+            }
+            if (ahead < a.top) best[ahead] = mine;
+        }
+        __syncthreads();
+    }
+    if (tid >= WAVE) return;
+    s = join_wave(s);
+    const float2 b = TOP && lane < a.top ? best[lane] : make_float2(0, __int_as_float(-1));
+    finish_row(a, row, s, b.x, __float_as_int(b.y), logit, token);
 }
 
 template <typename T, bool TOP> hipError_t logprobs_typed(const LogpArgs &a, hipStream_t st)
 {
     // short rows: a wavefront each
     if (a.vocab <= (int64_t)4 * WAVE * T::vec) {
-        logprob_kernel<T, 1, TOP><<<(unsigned)((a.rows + SEGS - 1) / SEGS), 256, 0, st>>>(a);
+        logprob_short<T, TOP><<<(unsigned)((a.rows + SEGS - 1) / SEGS), 256, 0, st>>>(a);
         return hipGetLastError();
     }
-    logprob_kernel<T, SEGS, TOP><<<(unsigned)(a.rows * a.splits), 256, 0, st>>>(a);
+    logprob_kernel<T, TOP><<<(unsigned)(a.rows * a.splits), 256, 0, st>>>(a);
     if (a.splits > 1) {
         if (hipError_t e = hipGetLastError()) return e;
-        logprob_join<T, TOP><<<(unsigned)a.rows, WAVE, 0, st>>>(a);
+        logprob_join<T, TOP><<<(unsigned)a.rows, 256, 0, st>>>(a);
     }
     return hipGetLastError();
 }
