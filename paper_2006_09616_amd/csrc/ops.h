@@ -13,7 +13,7 @@ constexpr int KEY_TILE = 64;      // keys of a tile of the attention kernels
 constexpr int ROW_TILE = 128;     // rows (queries x heads of a group) of a workgroup
 constexpr int FEW_ROWS = 32;      // rows of a key head that the kernel for few rows takes
 constexpr int GRAD_KEYS = 128;    // keys of a workgroup that sums dK and dV
-constexpr int SEGS = 4;           // segments of a row that a workgroup of the log-probability kernel reads
+constexpr int SEGS = 4;           // wavefronts of a workgroup of the log-probability kernel
 
 struct Heads {                    // [batch][position][head][head_dim], strides in elements
     char *data;

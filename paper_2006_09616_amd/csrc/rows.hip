@@ -283,32 +283,35 @@ __device__ void join_list(Top &top, float v, int32_t c, int k)
 
 constexpr int AHEAD = 4;
 
-// A wavefront's part of a row: whole 16-byte vectors v0 .. v1 - 1 of those
-// from `head` on, and elements before (at the row's start) and after them (at
-// its end), fewer than a vector's.
-template <typename T> struct Segment {
+// A wavefront's share of a row's part: chunks of four 16-byte vectors a lane,
+// the workgroup's WAVES wavefronts in turn, so that a workgroup reads one
+// stretch of memory.  Columns before the row's first 16-byte boundary go to
+// the first wavefront of the first part, those after its last whole vector to
+// the last of the last.
+template <typename T, int WAVES> struct Segment {
     using R = typename T::raw;
-    static constexpr int N = T::vec;
+    static constexpr int N = T::vec, CHUNK = AHEAD * WAVE, STEP = WAVES * CHUNK;
     const R *x;
-    int head, v0, v1, tail0, tails;      // columns 0 .. head - 1 if first, tail0 .. tail0 + tails - 1 if last
+    int head, part0, v0, v1, tail0, tails;
     bool first;
 
-    __device__ Segment(const R *row, int vocab, int seg, int segs) : x(row)
+    __device__ Segment(const R *row, int vocab, int wave, int part, int parts) : x(row)
     {
         const int mis = (int)((uintptr_t)row % 16 / sizeof(R));
         head = min(mis ? N - mis : 0, vocab);
-        const int vecs = (vocab - head) / N, per = (vecs + segs - 1) / segs;
-        v0 = min(per * seg, vecs);
-        v1 = min(v0 + per, vecs);
-        first = seg == 0;
+        const int vecs = (vocab - head) / N, per = parts > 1 ? (vecs + parts - 1) / parts : vecs;
+        part0 = min(per * part, vecs);
+        v0 = part0 + wave * CHUNK;
+        v1 = min(part0 + per, vecs);
+        first = part == 0 && wave == 0;
         tail0 = head + vecs * N;
-        tails = seg == segs - 1 ? vocab - tail0 : 0;
+        tails = part == parts - 1 && wave == WAVES - 1 ? vocab - tail0 : 0;
     }
     __device__ Pack<R, N> vector(int v) const { return *(const Pack<R, N> *)(x + head + (int64_t)v * N); }
 };
 
-template <typename T>
-__device__ __forceinline__ Stat segment_stat(const Segment<T> &g)
+template <typename T, int WAVES>
+__device__ __forceinline__ Stat segment_stat(const Segment<T, WAVES> &g)
 {
     using R = typename T::raw;
     constexpr int N = T::vec;
@@ -321,7 +324,7 @@ __device__ __forceinline__ Stat segment_stat(const Segment<T> &g)
             if (v + i * WAVE + lane < g.v1) ahead[i] = g.vector(v + i * WAVE + lane);
     };
     load(g.v0);
-    for (int v = g.v0; v < g.v1; v += AHEAD * WAVE) {
+    for (int v = g.v0; v < g.v1; v += g.STEP) {
         float e[AHEAD][N];
 #pragma unroll
         for (int i = 0; i < AHEAD; i++) {
@@ -329,7 +332,7 @@ __device__ __forceinline__ Stat segment_stat(const Segment<T> &g)
 #pragma unroll
             for (int j = 0; j < N; j++) e[i][j] = in ? (float)ahead[i].e[j] : -INFINITY;
         }
-        load(v + AHEAD * WAVE);
+        load(v + g.STEP);
 #pragma unroll
         for (int i = 0; i < AHEAD; i++) stat_step(s, e[i]);
     }
@@ -344,9 +347,9 @@ __device__ __forceinline__ Stat segment_stat(const Segment<T> &g)
     return s;
 }
 
-// The alternatives of a wavefront's segment, by the list.
-template <typename T>
-__device__ Top segment_top(const Segment<T> &g, int k)
+// The alternatives of a wavefront's share, by the list.
+template <typename T, int WAVES>
+__device__ Top segment_top(const Segment<T, WAVES> &g, int k)
 {
     constexpr int N = T::vec;
     const int lane = threadIdx.x % WAVE;
@@ -357,7 +360,8 @@ __device__ Top segment_top(const Segment<T> &g, int k)
         top_step(top, e, lane < n, c0 + lane, k);
     };
     if (g.first && g.head) edge(0, g.head);
-    for (int v = g.v0; v < g.v1; v += WAVE) {
+    for (int c = g.v0; c < g.v1; c += g.STEP)
+    for (int v = c; v < min(c + g.CHUNK, g.v1); v += WAVE) {
         const bool in = v + lane < g.v1;
         float e[N], most = -INFINITY;
         auto p = g.vector(in ? v + lane : v);
@@ -393,7 +397,7 @@ struct TopScratch {
 };
 
 template <typename T>
-__device__ void part_top(TopScratch &w, const Segment<T> &g, const typename T::raw *x, int vocab, int seg0, int segs, float most, int k)
+__device__ void part_top(TopScratch &w, const Segment<T, SEGS> &g, float most, int k)
 {
     constexpr int N = T::vec;
     const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE;
@@ -402,6 +406,7 @@ __device__ void part_top(TopScratch &w, const Segment<T> &g, const typename T::r
     if (tid < 32) w.best[tid] = make_float2(0, __int_as_float(-1));
     __syncthreads();
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < 256; j += 4) {
         const float4 o = *(const float4 *)&w.most[j];
         rank += (o.x > most || (o.x == most && j < tid)) + (o.y > most || (o.y == most && j + 1 < tid)) +
@@ -416,18 +421,16 @@ __device__ void part_top(TopScratch &w, const Segment<T> &g, const typename T::r
         const int at = atomicAdd(&w.n_found, 1);
         if (at < FOUND) w.found[at] = make_float2(v, __int_as_float(c));
     };
-    if (g.first && lane < g.head) offer((float)x[lane], lane);
-    if (lane < g.tails) offer((float)x[g.tail0 + lane], g.tail0 + lane);
+    if (g.first && lane < g.head) offer((float)g.x[lane], lane);
+    if (lane < g.tails) offer((float)g.x[g.tail0 + lane], g.tail0 + lane);
     __syncthreads();
-    // all lanes with equal maxima: as many lanes' columns as the row has
-    const int vecs = (vocab - g.head) / N, per = (vecs + segs - 1) / segs, each = (per + WAVE - 1) / WAVE;
+    const int each = (g.v1 - g.part0 + g.STEP - 1) / g.STEP * AHEAD;       // vectors of a lane, at most
     const int n_lanes = w.n_lanes;
     if (n_lanes <= 4 * k)
         for (int i = tid; i < n_lanes * each; i += 256) {
-            const int owner = w.lanes[i / each];
-            const int begin = min(per * (seg0 + owner / WAVE), vecs), end = min(begin + per, vecs);
-            const int v = begin + owner % WAVE + i % each * WAVE;
-            if (v >= end) continue;
+            const int owner = w.lanes[i / each], n = i % each;
+            const int v = g.part0 + n / AHEAD * g.STEP + owner / WAVE * g.CHUNK + n % AHEAD * WAVE + owner % WAVE;
+            if (v >= g.v1) continue;
             const auto p = g.vector(v);
 #pragma unroll
             for (int e = 0; e < N; e++) offer((float)p.e[e], g.head + v * N + e);
@@ -438,6 +441,7 @@ __device__ void part_top(TopScratch &w, const Segment<T> &g, const typename T::r
         for (int i = tid; i < n; i += 256) {
             const float2 mine = w.found[i];
             int ahead = 0;
+#pragma unroll 8
             for (int j = 0; j < n; j++) {
                 const float2 o = w.found[j];
                 ahead += o.x > mine.x || (o.x == mine.x && __float_as_int(o.y) < __float_as_int(mine.y));
@@ -445,7 +449,7 @@ __device__ void part_top(TopScratch &w, const Segment<T> &g, const typename T::r
             if (ahead < k) w.best[ahead] = mine;
         }
     } else {
-        Top top = segment_top<T>(g, k);
+        Top top = segment_top<T, SEGS>(g, k);
         if (lane < k) w.lists[wave][lane] = make_float2(top.value, __int_as_float(top.column));
         __syncthreads();
         if (wave == 0) {
@@ -469,15 +473,15 @@ __global__ void __launch_bounds__(256) logprob_short(LogpArgs a)
     const R *x = (const R *)a.x + row * a.stride;
     const int64_t token = a.tokens[row];
     const float logit = token >= 0 && token < a.vocab ? (float)x[token] : 0.0f;
-    const Segment<T> g(x, (int)a.vocab, 0, 1);
-    const Stat s = join_wave(segment_stat<T>(g));
+    const Segment<T, 1> g(x, (int)a.vocab, 0, 0, 1);
+    const Stat s = join_wave(segment_stat<T, 1>(g));
     Top top;
     top.clear();
-    if (TOP) top = segment_top<T>(g, a.top);
+    if (TOP) top = segment_top<T, 1>(g, a.top);
     finish_row(a, row, s, top.value, top.column, logit, token);
 }
 
-// A workgroup a row, or a part of one; a contiguous segment for each wavefront.
+// A workgroup a row, or a part of one.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(256) logprob_kernel(LogpArgs a)
 {
@@ -489,9 +493,8 @@ __global__ void __launch_bounds__(256) logprob_kernel(LogpArgs a)
     const R *x = (const R *)a.x + row * a.stride;
     const int64_t token = a.tokens[row];
     const float logit = token >= 0 && token < a.vocab ? (float)x[token] : 0.0f;
-    const int seg0 = split * SEGS, segs = a.splits * SEGS;
-    const Segment<T> g(x, (int)a.vocab, seg0 + __builtin_amdgcn_readfirstlane(wave), segs);
-    Stat s = segment_stat<T>(g);
+    const Segment<T, SEGS> g(x, (int)a.vocab, __builtin_amdgcn_readfirstlane(wave), split, a.splits);
+    Stat s = segment_stat<T, SEGS>(g);
     const float most = s.m;
     s = join_wave(s);
     if (lane == 0) {
@@ -499,7 +502,7 @@ __global__ void __launch_bounds__(256) logprob_kernel(LogpArgs a)
         part[wave][1] = s.l;
         part[wave][2] = s.w;
     }
-    if (TOP) part_top<T>(scratch, g, x, (int)a.vocab, seg0, segs, most, a.top);
+    if (TOP) part_top<T>(scratch, g, most, a.top);
     else __syncthreads();
     if (wave) return;
     s = {part[0][0], part[0][1], part[0][2]};
@@ -544,6 +547,7 @@ __global__ void __launch_bounds__(256) logprob_join(LogpArgs a)
             const float2 mine = all[i];
             if (__float_as_int(mine.y) < 0) continue;
             int ahead = 0;
+#pragma unroll 8
             for (int j = 0; j < n; j++) {
                 const float2 o = all[j];
                 ahead += __float_as_int(o.y) >= 0 &&
