@@ -71,7 +71,7 @@ typedef struct {
 
 /* A tensor [batch][position][head][head_dim]: strides in elements, the last
  * dimension contiguous; data 16-byte aligned and strides multiples of 8,
- * that of positions below 2^26.  Input strides may be 0 (broadcast). */
+ * that of positions below 2^24.  Input strides may be 0 (broadcast). */
 typedef struct {
     void *data;
     int64_t batch, position, head;

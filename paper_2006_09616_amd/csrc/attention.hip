@@ -95,40 +95,51 @@ template <int NB> struct Tile {
     }
 };
 
-// 64 rows of a tensor (consecutive positions of a head) on their way to LDS,
-// 256 threads; rows from `end` on and columns from head_dim on are zero.  The
-// address is a uniform base and a 32-bit offset of the lane.
+// Moves 64 rows of a tensor (consecutive positions of a head) from memory into
+// a tile in LDS without passing through registers, 256 threads.  Each
+// instruction of a wavefront fills 1024 bytes of the tile in order, lane by
+// lane; the swizzle is in the addresses that the lanes read.  Reads go through
+// a buffer descriptor of the rows up to `end`: beyond them, and for columns
+// from head_dim on, it delivers zeros.  The compiler does not see these loads:
+// moved() waits for them, before the barrier that hands the tile over.
 constexpr int STAGE_ROWS = 64;
+static_assert(STAGE_ROWS == KEY_TILE, "a tile of keys is moved at once");
 
-template <int NB> struct Staged {
+__device__ __forceinline__ uint32_t lds_address(const void *p)
+{
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p);
+}
+
+__device__ __forceinline__ void moved() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// For the compiler: nothing that was loaded before the loop is pending within.
+__device__ __forceinline__ void ready() { __builtin_amdgcn_s_waitcnt(0); }
+
+template <int NB> struct Mover {
     using L = Tile<NB>;
-    static constexpr int N = STAGE_ROWS * L::CHUNKS / 256, STEP = 256 / L::CHUNKS;
-    uint4 r[N];
-    __device__ void load(const char *base, int64_t stride, int row0, int end, int head_dim)
+    static constexpr int PER = 64 / L::CHUNKS, N = STAGE_ROWS / PER / 4;      // rows an instruction, instructions a wavefront
+    uint32_t offset, bytes, step;
+    __device__ Mover(int64_t stride, int head_dim)
     {
-        const int c = threadIdx.x % L::CHUNKS, i = threadIdx.x / L::CHUNKS;
-        const char *p = base + row0 * stride * 2;
-        const uint32_t off = (uint32_t)(i * (uint32_t)stride + c * 8) * 2u;
-#pragma unroll
-        for (int n = 0; n < N; n++) r[n] = make_uint4(0, 0, 0, 0);
-        if (c * 8 >= head_dim) return;
-        if (row0 + STAGE_ROWS <= end) {
-#pragma unroll
-            for (int n = 0; n < N; n++) r[n] = *(const uint4 *)(p + n * STEP * stride * 2 + off);
-        } else {
-#pragma unroll
-            for (int n = 0; n < N; n++)
-                if (row0 + i + n * STEP < end) r[n] = *(const uint4 *)(p + n * STEP * stride * 2 + off);
-        }
+        const int lane = threadIdx.x % WAVE, row = threadIdx.x / WAVE * PER + lane / L::CHUNKS;
+        const int chunk = lane % L::CHUNKS ^ L::swizzle(row);                   // the same 4 PER rows further on
+        bytes = (uint32_t)stride * 2u;
+        step = 4 * PER * bytes;
+        offset = chunk * 8 < head_dim ? row * bytes + chunk * 16 : 0x80000000u;
     }
-    __device__ void store(short *tile) const
+    __device__ void load(short *tile, const char *base, int row0, int end, int head_dim) const
     {
-        const int c = threadIdx.x % L::CHUNKS, i = threadIdx.x / L::CHUNKS;
+        const uint64_t p = (uint64_t)(base + (int64_t)row0 * bytes);
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        const u32x4 rsrc = {(uint32_t)p, (uint32_t)(p >> 32), (uint32_t)(min(end - row0, STAGE_ROWS) - 1) * bytes + head_dim * 2,
+                            0x00027000u};
+        const uint32_t at = lds_address(tile) + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) * 1024;
 #pragma unroll
-        for (int n = 0; n < N; n++) *(uint4 *)(tile + L::at(i + n * STEP, c)) = r[n];
+        for (int n = 0; n < N; n++)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                         :: "s"(at + n * 4096), "v"(offset + n * step), "s"(rsrc) : "memory", "m0");
     }
 };
-static_assert(STAGE_ROWS == KEY_TILE, "a tile of keys is staged at once");
 
 // Rows of one key head in packed order: row = query * group + head of the
 // group, so that a tile holds the group's heads of few queries and reads the
@@ -283,9 +294,15 @@ template <int ROWS, int THREADS> struct RowBlock {
         }
         return w;
     }
-    __device__ bool sees(const AttnArgs &a, int key) const
+    // x = other for the lane's keys (key0 + 32 (i / 16) + 8 (i % 16 / 4) + i % 4) that its row does not see
+    template <int N> __device__ void mask(const AttnArgs &a, float (&x)[N], int key0, float other) const
     {
-        return key < end && (!u.docs || u.docs[min(key, a.k_len - 1)] == doc);
+#pragma unroll
+        for (int i = 0; i < N; i++) x[i] = key0 + 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4 < end ? x[i] : other;
+        if (!u.docs) return;
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            x[i] = u.docs[min(key0 + 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4, a.k_len - 1)] == doc ? x[i] : other;
     }
 };
 
@@ -321,8 +338,8 @@ struct Shape {
 
 // ---- forward -----------------------------------------------------------------
 // A workgroup has 128 rows, a wavefront 32, and walks over tiles of 64 keys.
-// The next tile is on its way from memory to registers while one is worked
-// on in LDS (two buffers, one barrier a tile).
+// The next tile is on its way from memory while one is worked on (two buffers,
+// one barrier a tile).
 
 template <typename T, int NB, bool SHAPED>
 __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
@@ -365,40 +382,49 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
     const char *kb = head_base(a.k, u.b, u.g), *vb = head_base(a.v, u.b, u.g);
 
     int t = w.next(w.t0);
-    Staged<NB> sk, sv;
+    const Mover<NB> mk(a.k.position, a.head_dim), mv(a.v.position, a.head_dim);
     if (t < w.t1) {
-        sk.load(kb, a.k.position, t * KEY_TILE, u.len, a.head_dim);
-        sv.load(vb, a.v.position, t * KEY_TILE, u.len, a.head_dim);
-        sk.store(tiles);
-        sv.store(tiles + 2 * SIZE);
+        mk.load(tiles, kb, t * KEY_TILE, u.len, a.head_dim);
+        mv.load(tiles + 2 * SIZE, vb, t * KEY_TILE, u.len, a.head_dim);
     }
+    moved();
+    ready();
     __syncthreads();
     for (int buf = 0; t < w.t1; buf ^= 1) {
         const int j0 = t * KEY_TILE, t2 = w.next(t + 1);
         if (t2 < w.t1) {
-            sk.load(kb, a.k.position, t2 * KEY_TILE, u.len, a.head_dim);
-            sv.load(vb, a.v.position, t2 * KEY_TILE, u.len, a.head_dim);
+            mk.load(tiles + (buf ^ 1) * SIZE, kb, t2 * KEY_TILE, u.len, a.head_dim);
+            mv.load(tiles + (2 + (buf ^ 1)) * SIZE, vb, t2 * KEY_TILE, u.len, a.head_dim);
         }
         if (j0 < w.wave_end) {
             const short *ks = tiles + buf * SIZE;
             short *vs = tiles + (2 + buf) * SIZE;
+            // operands are read from LDS a group of products ahead
             f32x16 s[2] = {};
+            s16x8 f[2][4];
+            auto keys = [&](int g) {
 #pragma unroll
-            for (int st = 0; st < 2 * NB; st++)
+                for (int n = 0; n < 4; n++) f[g & 1][n] = L::row_operand(ks, 32 * (n & 1) + lane % 32, 2 * g + n / 2);
+            };
+            auto values = [&](int kc) {
 #pragma unroll
-                for (int kb2 = 0; kb2 < 2; kb2++)
-                    s[kb2] = T::mfma(L::row_operand(ks, 32 * kb2 + lane % 32, st), q[st], s[kb2]);
+                for (int d = 0; d < NB; d++) f[kc & 1][d] = L::column_operand(vs, 16 * kc, d);
+            };
+            keys(0);
+#pragma unroll
+            for (int g = 0; g < NB; g++) {
+                if (g + 1 < NB) keys(g + 1);
+#pragma unroll
+                for (int n = 0; n < 4; n++) s[n & 1] = T::mfma(f[g & 1][n], q[2 * g + n / 2], s[n & 1]);
+            }
+            values(0);
             // x: the scores times log2(e); plain ones but for a factor left to the exponent's fma
             float x[32];
             const float gain = SHAPED ? 1.0f : shape.scale2;
 #pragma unroll
             for (int i = 0; i < 32; i++) x[i] = s[i / 16][i % 16];
             if (SHAPED) shape.apply(x, w.pos - j0 - 4 * hi);
-            if (!w.whole(t)) {
-#pragma unroll
-                for (int i = 0; i < 32; i++)
-                    x[i] = w.sees(a, j0 + 4 * hi + 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4) ? x[i] : -INFINITY;
-            }
+            if (!w.whole(t)) w.mask(a, x, j0 + 4 * hi, -INFINITY);
             float most = x[0];
 #pragma unroll
             for (int i = 1; i < 32; i++) most = fmaxf(most, x[i]);
@@ -421,14 +447,12 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
 #pragma unroll
             for (int kc = 0; kc < 4; kc++) {
                 const s16x8 p = rounded<T>(x + 8 * kc);
+                if (kc < 3) values(kc + 1);
 #pragma unroll
-                for (int d = 0; d < NB; d++) o[d] = T::mfma(L::column_operand(vs, 16 * kc, d), p, o[d]);
+                for (int d = 0; d < NB; d++) o[d] = T::mfma(f[kc & 1][d], p, o[d]);
             }
         }
-        if (t2 < w.t1) {
-            sk.store(tiles + (buf ^ 1) * SIZE);
-            sv.store(tiles + (2 + (buf ^ 1)) * SIZE);
-        }
+        moved();
         __syncthreads();
         t = t2;
     }
@@ -557,10 +581,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
 #pragma unroll
         for (int i = 0; i < 16; i++) x[i] = s[i];
         if (SHAPED) shape.apply(x, w.pos - j0 - 4 * hi);
-        if (j0 + FEW_KEYS > w.sure || u.docs) {
-#pragma unroll
-            for (int i = 0; i < 16; i++) x[i] = w.sees(a, j0 + 4 * hi + 8 * (i / 4) + i % 4) ? x[i] : -INFINITY;
-        }
+        if (j0 + FEW_KEYS > w.sure || u.docs) w.mask(a, x, j0 + 4 * hi, -INFINITY);
         float most = x[0];
 #pragma unroll
         for (int i = 1; i < 16; i++) most = fmaxf(most, x[i]);
@@ -746,19 +767,19 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
     const char *kb = head_base(a.k, u.b, u.g), *vb = head_base(a.v, u.b, u.g);
 
     int t = w.next(w.t0);
-    Staged<NB> sk, sv;
+    const Mover<NB> mk(a.k.position, a.head_dim), mv(a.v.position, a.head_dim);
     if (t < w.t1) {
-        sk.load(kb, a.k.position, t * KEY_TILE, u.len, a.head_dim);
-        sv.load(vb, a.v.position, t * KEY_TILE, u.len, a.head_dim);
-        sk.store(tiles);
-        sv.store(tiles + 2 * SIZE);
+        mk.load(tiles, kb, t * KEY_TILE, u.len, a.head_dim);
+        mv.load(tiles + 2 * SIZE, vb, t * KEY_TILE, u.len, a.head_dim);
     }
+    moved();
+    ready();
     __syncthreads();
     for (int buf = 0; t < w.t1; buf ^= 1) {
         const int j0 = t * KEY_TILE, t2 = w.next(t + 1);
         if (t2 < w.t1) {
-            sk.load(kb, a.k.position, t2 * KEY_TILE, u.len, a.head_dim);
-            sv.load(vb, a.v.position, t2 * KEY_TILE, u.len, a.head_dim);
+            mk.load(tiles + (buf ^ 1) * SIZE, kb, t2 * KEY_TILE, u.len, a.head_dim);
+            mv.load(tiles + (2 + (buf ^ 1)) * SIZE, vb, t2 * KEY_TILE, u.len, a.head_dim);
         }
         if (j0 < w.wave_end) {
             short *ks = tiles + buf * SIZE;
@@ -794,11 +815,7 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
                 }
 #pragma unroll
                 for (int i = 0; i < 16; i++) x[i] *= exp2_(y[i]);
-                if (!whole) {
-#pragma unroll
-                    for (int i = 0; i < 16; i++)
-                        x[i] = w.sees(a, j0 + 32 * kb2 + 4 * hi + 8 * (i / 4) + i % 4) ? x[i] : 0.0f;
-                }
+                if (!whole) w.mask(a, x, j0 + 32 * kb2 + 4 * hi, 0.0f);
 #pragma unroll
                 for (int kc = 0; kc < 2; kc++) {
                     const s16x8 p = rounded<T>(x + 8 * kc);
@@ -807,10 +824,7 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
                 }
             }
         }
-        if (t2 < w.t1) {
-            sk.store(tiles + (buf ^ 1) * SIZE);
-            sv.store(tiles + (2 + (buf ^ 1)) * SIZE);
-        }
+        moved();
         __syncthreads();
         t = t2;
     }
@@ -894,13 +908,13 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
             }
         return i;
     };
-    Staged<NB> sq, sg;
+    const Mover<NB> mq(a.q.position, a.head_dim), mg(a.dout.position, a.head_dim);
     float2 stat;
     int rdoc = 0;
-    auto load = [&](int i) {
+    auto load = [&](int i, int buf) {
         const int head = u.g * a.group + i / tiles_q, q0 = query_of(i);
-        sq.load(head_base(a.q, u.b, head), a.q.position, q0, a.q_len, a.head_dim);
-        sg.load(head_base(a.dout, u.b, head), a.dout.position, q0, a.q_len, a.head_dim);
+        mq.load(tiles + buf * SIZE, head_base(a.q, u.b, head), q0, a.q_len, a.head_dim);
+        mg.load(tiles + (2 + buf) * SIZE, head_base(a.dout, u.b, head), q0, a.q_len, a.head_dim);
         if (threadIdx.x < ROWS) {
             const int query = q0 + threadIdx.x, pos = u.start + query;
             stat = query < a.q_len ? a.row_stat[((int64_t)u.b * a.k_heads * a.group + head) * a.q_len + query]
@@ -913,8 +927,6 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
         }
     };
     auto store = [&](int buf) {
-        sq.store(tiles + buf * SIZE);
-        sg.store(tiles + (2 + buf) * SIZE);
         if (threadIdx.x < ROWS) {
             lse2s[buf][threadIdx.x] = stat.x - T::p_shift;
             deltas[buf][threadIdx.x] = stat.y * (1.0f / T::p_gain);
@@ -924,13 +936,15 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
 
     int i = next(i0);
     if (i < i1) {
-        load(i);
+        load(i, 0);
         store(0);
     }
+    moved();
+    ready();
     __syncthreads();
     for (int buf = 0; i < i1; buf ^= 1) {
         const int i2 = next(i + 1), q0 = query_of(i);
-        if (i2 < i1) load(i2);
+        if (i2 < i1) load(i2, buf ^ 1);
         bool in_doc = true;
         if (u.docs) {
             const int2 d = row_docs(q0);
@@ -1001,6 +1015,7 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
             }
         }
         if (i2 < i1) store(buf ^ 1);
+        moved();
         __syncthreads();
         i = i2;
     }

@@ -16,7 +16,7 @@ using namespace dtrops;
 namespace {
 
 constexpr int32_t MAX_LEN = 1 << 24;
-constexpr int64_t MAX_STRIDE = int64_t(1) << 26; // between positions: 32-bit offsets within 16 of them
+constexpr int64_t MAX_STRIDE = int64_t(1) << 24; // between positions: 64 of them within 2^31 bytes
 constexpr int64_t MAX_ROWS = int64_t(1) << 31;
 constexpr int64_t MAX_GROUPS = int64_t(1) << 24;   // workgroups of a launch: 2^32 work items
 
