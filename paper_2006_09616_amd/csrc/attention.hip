@@ -9,6 +9,8 @@
 // a product may run over its keys in any order, so V^T is read (transposed,
 // from LDS) in the order in which the lane holds its keys.  Backward does the
 // same with the roles of queries and keys exchanged where needed.
+#include <type_traits>
+
 #include "ops.h"
 
 namespace dtrops {
@@ -52,6 +54,38 @@ template <typename T> __device__ __forceinline__ s16x8 rounded(const float *p)
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = (typename T::raw)p[i];
     return __builtin_bit_cast(s16x8, v);
+}
+
+// f of the numbers I .. N - 1, each a constant of its own type
+template <int I, int N, typename F> __device__ __forceinline__ void static_for(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<I + 1, N>(f);
+    }
+}
+
+// Order for the scheduler: READS reads of LDS first, then TIMES times one
+// matrix instruction, EACH reads and VALUS vector instructions.
+template <int READS, int TIMES, int EACH, int VALUS> __device__ __forceinline__ void interleave()
+{
+    if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+#pragma unroll
+    for (int i = 0; i < TIMES; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (EACH > 0) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+        if constexpr (VALUS > 0) __builtin_amdgcn_sched_group_barrier(0x002, VALUS, 0);
+    }
+}
+
+// two numbers rounded into an operand's elements i and i + 1
+template <typename T> __device__ __forceinline__ void put_two(s16x8 &v, int i, const float (&x)[2])
+{
+    typedef typename T::raw r2 __attribute__((ext_vector_type(2)));
+    typedef short s2 __attribute__((ext_vector_type(2)));
+    const s2 b = __builtin_bit_cast(s2, r2{(typename T::raw)x[0], (typename T::raw)x[1]});
+    v[i] = b[0];
+    v[i + 1] = b[1];
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -418,6 +452,8 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
                 for (int n = 0; n < 4; n++) s[n & 1] = T::mfma(f[g & 1][n], q[2 * g + n / 2], s[n & 1]);
             }
             values(0);
+            interleave<8, 2 * NB * 2 - 8, 1, 0>();
+            interleave<0, 8, 1, 0>();
             // x: the scores times log2(e); plain ones but for a factor left to the exponent's fma
             float x[32];
             const float gain = SHAPED ? 1.0f : shape.scale2;
@@ -843,8 +879,8 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 // of one head after the other of the group (two buffers in LDS, one barrier a
 // step).  Where key blocks are few, the steps are cut into parts whose sums
 // are added up by grad_join_kernel.
-template <typename T, int NB, bool SHAPED>
-__global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
+template <typename T, int NB, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
     constexpr int ROWS = STAGE_ROWS, SIZE = ROWS * L::PITCH;
@@ -874,8 +910,7 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
         }
     }
     const int kdoc = u.docs ? u.docs[min(key, a.k_len - 1)] : 0;
-    const bool capped = a.cap > 0, bias = a.slopes != nullptr;
-    const float scale2 = capped ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    const float scale2 = CAP ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
     f32x16 dk[NB] = {}, dv[NB] = {};
 
     // queries that may see any of the keys: from `first` on, `tiles_q` steps a head
@@ -892,7 +927,18 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
         i0 = min(per * part, i1);
         i1 = min(i0 + per, i1);
     }
-    auto query_of = [&](int i) { return first + i % tiles_q * ROWS; };
+    // a step: number i, 64 queries from q0 on of one head of the group
+    struct Step { int i, head, q0; };
+    auto step_at = [&](int i) { return Step{i, tiles_q ? i / tiles_q : 0, tiles_q ? first + i % tiles_q * ROWS : 0}; };
+    auto after = [&](Step s) {
+        s.i++;
+        s.q0 += ROWS;
+        if (s.q0 >= a.q_len) {
+            s.q0 = first;
+            s.head++;
+        }
+        return s;
+    };
     // documents of a step's queries, as the (at most two) tiles of their positions give them
     auto row_docs = [&](int q0) {
         const int p0 = max(u.start + q0, 0), p1 = min(u.start + min(q0 + ROWS, a.q_len) - 1, a.k_len - 1);
@@ -900,23 +946,31 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
         const int2 x = u.doc_tiles[p0 / KEY_TILE], y = u.doc_tiles[p1 / KEY_TILE];
         return make_int2(min(x.x, y.x), max(x.y, y.y));
     };
-    auto next = [&](int i) {
-        if (u.docs)
-            for (; i < i1; i++) {
-                const int2 d = row_docs(query_of(i));
-                if (d.x <= doc_hi && d.y >= doc_lo) break;
+    auto same_doc = [&](int q0) {
+        if (!u.docs) return true;
+        const int2 d = row_docs(q0);
+        return d.x == d.y && doc_lo == doc_hi && u.start + q0 >= 0 && u.start + min(q0 + ROWS, a.q_len) <= a.k_len;
+    };
+    // every query of the step sees every key of the workgroup
+    auto whole_step = [&](int q0) { return j0 + GRAD_KEYS <= u.end(a, u.start + q0) && q0 + ROWS <= a.q_len && same_doc(q0); };
+    // the first step from s on that has work, of the kind asked for: 0 not whole, 1 whole, 2 either
+    auto next = [&](Step s, int kind) {
+        for (; s.i < i1; s = after(s)) {
+            if (u.docs) {
+                const int2 d = row_docs(s.q0);
+                if (d.x > doc_hi || d.y < doc_lo) continue;
             }
-        return i;
+            if (kind == 2 || (int)whole_step(s.q0) == kind) break;
+        }
+        return s;
     };
     const Mover<NB> mq(a.q.position, a.head_dim), mg(a.dout.position, a.head_dim);
     float2 stat;
     int rdoc = 0;
-    auto load = [&](int i, int buf) {
-        const int head = u.g * a.group + i / tiles_q, q0 = query_of(i);
-        mq.load(tiles + buf * SIZE, head_base(a.q, u.b, head), q0, a.q_len, a.head_dim);
-        mg.load(tiles + (2 + buf) * SIZE, head_base(a.dout, u.b, head), q0, a.q_len, a.head_dim);
+    auto load = [&](const Step &s, int buf) {
+        const int head = u.g * a.group + s.head;
         if (threadIdx.x < ROWS) {
-            const int query = q0 + threadIdx.x, pos = u.start + query;
+            const int query = s.q0 + threadIdx.x, pos = u.start + query;
             stat = query < a.q_len ? a.row_stat[((int64_t)u.b * a.k_heads * a.group + head) * a.q_len + query]
                                    : make_float2(INFINITY, 0.0f);
             if (u.docs) {
@@ -925,6 +979,8 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
                 else stat.x = INFINITY;
             }
         }
+        mq.load(tiles + buf * SIZE, head_base(a.q, u.b, head), s.q0, a.q_len, a.head_dim);
+        mg.load(tiles + (2 + buf) * SIZE, head_base(a.dout, u.b, head), s.q0, a.q_len, a.head_dim);
     };
     auto store = [&](int buf) {
         if (threadIdx.x < ROWS) {
@@ -933,73 +989,55 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
             docs[buf][threadIdx.x] = rdoc;
         }
     };
-
-    int i = next(i0);
-    if (i < i1) {
-        load(i, 0);
-        store(0);
-    }
-    moved();
-    ready();
-    __syncthreads();
-    for (int buf = 0; i < i1; buf ^= 1) {
-        const int i2 = next(i + 1), q0 = query_of(i);
-        if (i2 < i1) load(i2, buf ^ 1);
-        bool in_doc = true;
-        if (u.docs) {
-            const int2 d = row_docs(q0);
-            in_doc = d.x == d.y && doc_lo == doc_hi && u.start + q0 >= 0 && u.start + min(q0 + ROWS, a.q_len) <= a.k_len;
+    // probability and score gradient of one element: query qi of the step, of scores s and dP dp
+    auto element = [&](float distance, float slope2, float s, float dp, float lse2, float delta, float &p, float &ds)
+                       __attribute__((always_inline)) {
+        ds = fmaf(dp, 1.0f / T::p_gain, -delta);
+        float y;
+        if constexpr (CAP) {
+            const float th = tanh_of(s * scale2);
+            y = fmaf(cap2, th, -lse2);
+            ds *= fmaf(-th, th, 1.0f);
+        } else {
+            y = fmaf(s, scale2, -lse2);
         }
-        const float slope2 = SHAPED && bias ? a.slopes[u.g * a.group + i / tiles_q] * LOG2E : 0.0f;
+        if (BIAS) y -= slope2 * fabsf(distance);
+        p = exp2_(y);
+        ds *= p;
+    };
+
+    // A step, 32 queries after the other, whatever the masks.
+    auto any_step = [&](const Step &st, int buf) {
+        const bool in_doc = same_doc(st.q0);
+        const float slope2 = BIAS ? a.slopes[u.g * a.group + st.head] * LOG2E : 0.0f;
 #pragma unroll 1
         for (int sb = 0; sb < 2; sb++) {
-            const int qs0 = q0 + 32 * sb, p0 = u.start + qs0;                  // the first of 32 queries
-            if (qs0 >= a.q_len || jw >= u.end(a, p0 + 31)) continue;
-            const bool whole = in_doc && jw + 32 <= u.end(a, p0);
-            short *qt = tiles + buf * SIZE + 32 * sb * L::PITCH, *gt = tiles + (2 + buf) * SIZE + 32 * sb * L::PITCH;
+            const int pb = u.start + st.q0 + 32 * sb;
+            if (st.q0 + 32 * sb >= a.q_len || jw >= u.end(a, pb + 31)) continue;
+            short *const qh = tiles + buf * SIZE + 32 * sb * L::PITCH, *const gh = tiles + (2 + buf) * SIZE + 32 * sb * L::PITCH;
             f32x16 s = {}, dp = {};
 #pragma unroll
-            for (int st = 0; st < 2 * NB; st++) {
-                s = T::mfma(L::row_operand(qt, lane % 32, st), kf[st], s);
-                dp = T::mfma(L::row_operand(gt, lane % 32, st), vf[st], dp);
+            for (int k = 0; k < 2 * NB; k++) {
+                s = T::mfma(L::row_operand(qh, lane % 32, k), kf[k], s);
+                dp = T::mfma(L::row_operand(gh, lane % 32, k), vf[k], dp);
             }
             float p[16], ds[16];
+            const float d0 = (float)(key - pb - 4 * hi);
 #pragma unroll
             for (int e = 0; e < 4; e++) {
                 const f32x4 lse2 = *(const f32x4 *)&lse2s[buf][32 * sb + 8 * e + 4 * hi];
                 const f32x4 delta = *(const f32x4 *)&deltas[buf][32 * sb + 8 * e + 4 * hi];
-                if (SHAPED && capped) {
 #pragma unroll
-                    for (int n = 0; n < 4; n++) {
-                        const float th = tanh_of(s[4 * e + n] * scale2);
-                        p[4 * e + n] = fmaf(cap2, th, -lse2[n]);
-                        ds[4 * e + n] = fmaf(dp[4 * e + n], 1.0f / T::p_gain, -delta[n]) * fmaf(-th, th, 1.0f);
-                    }
-                } else {
-#pragma unroll
-                    for (int n = 0; n < 4; n++) {
-                        p[4 * e + n] = fmaf(s[4 * e + n], scale2, -lse2[n]);
-                        ds[4 * e + n] = fmaf(dp[4 * e + n], 1.0f / T::p_gain, -delta[n]);
-                    }
-                }
+                for (int n = 0; n < 4; n++)
+                    element(d0 - (float)(8 * e + n), slope2, s[4 * e + n], dp[4 * e + n], lse2[n], delta[n], p[4 * e + n], ds[4 * e + n]);
             }
-            if (SHAPED && bias) {
-                const float kf0 = (float)(key - p0 - 4 * hi);
-#pragma unroll
-                for (int n = 0; n < 16; n++) p[n] -= slope2 * fabsf(kf0 - (float)(8 * (n / 4) + n % 4));
-            }
-#pragma unroll
-            for (int n = 0; n < 16; n++) {
-                p[n] = exp2_(p[n]);
-                ds[n] *= p[n];
-            }
-            if (!whole) {
+            if (!in_doc || jw + 32 > u.end(a, pb)) {
                 // queries of the 32 that see the key: from `from` on
-                const int from = key >= u.len ? INT32_MAX : a.causal && key >= u.prefix ? key - p0 - 4 * hi : INT32_MIN;
+                const int from = key >= u.len ? INT32_MAX : a.causal && key >= u.prefix ? key - pb - 4 * hi : INT32_MIN;
 #pragma unroll
                 for (int n = 0; n < 16; n++) {
                     const int r = 8 * (n / 4) + n % 4;
-                    const bool seen = r >= from && (!u.docs || docs[buf][32 * sb + 4 * hi + r] == kdoc);
+                    const bool seen = (r >= from) & (docs[buf][32 * sb + 4 * hi + r] == kdoc);
                     p[n] = seen ? p[n] : 0.0f;
                     ds[n] = seen ? ds[n] : 0.0f;
                 }
@@ -1009,15 +1047,92 @@ __global__ void __launch_bounds__(256, 1) dkv_kernel(AttnArgs a)
                 const s16x8 pr = rounded<T>(p + 8 * kc), dr = rounded<T>(ds + 8 * kc);
 #pragma unroll
                 for (int d = 0; d < NB; d++) {
-                    dv[d] = T::mfma(L::column_operand(gt, 16 * kc, d), pr, dv[d]);
-                    dk[d] = T::mfma(L::column_operand(qt, 16 * kc, d), dr, dk[d]);
+                    dv[d] = T::mfma(L::column_operand(gh, 16 * kc, d), pr, dv[d]);
+                    dk[d] = T::mfma(L::column_operand(qh, 16 * kc, d), dr, dk[d]);
                 }
             }
         }
-        if (i2 < i1) store(buf ^ 1);
+    };
+
+    // A step whose queries all see all keys: both halves in one stretch of
+    // code.  Its matrix instructions, in order: scores and dP of the halves,
+    // then their sums; operands are read from LDS six instructions ahead, and
+    // the elements of a half are worked out between the matrix instructions of
+    // the next stage.
+    auto whole = [&](const Step &st, int buf) __attribute__((always_inline)) {
+        constexpr int M = 4 * NB, AHEAD = 6;              // matrix instructions of a stage
+        short *const qt = tiles + buf * SIZE, *const gt = tiles + (2 + buf) * SIZE;
+        const float slope2 = BIAS ? a.slopes[u.g * a.group + st.head] * LOG2E : 0.0f;
+        const float d0 = (float)(key - u.start - st.q0 - 4 * hi);
+        f32x16 s[2] = {}, dp[2] = {};
+        f32x4 lse2[2], delta[2];                          // of four queries, and of the next four
+        float p[2], ds[2];
+        s16x8 pr[2][2], dr[2][2], ring[AHEAD];
+        auto operand = [&](auto at) __attribute__((always_inline)) {
+            constexpr int i = at, sb = i / M % 2, j = i % M;
+            if constexpr (i < 2 * M) return L::row_operand((j & 1 ? gt : qt) + 32 * sb * L::PITCH, lane % 32, j / 2);
+            else return L::column_operand((j & 1 ? qt : gt) + 32 * sb * L::PITCH, 16 * (j / (2 * NB)), j / 2 % NB);
+        };
+        auto row_stats = [&](int four) __attribute__((always_inline)) {
+            lse2[four % 2] = *(const f32x4 *)&lse2s[buf][8 * four + 4 * hi];
+            delta[four % 2] = *(const f32x4 *)&deltas[buf][8 * four + 4 * hi];
+        };
+        static_for<0, AHEAD>([&](auto at) __attribute__((always_inline)) { ring[at] = operand(at); });
+        row_stats(0);
+        static_for<0, 4 * M>([&](auto at) __attribute__((always_inline)) {
+            constexpr int i = at, sb = i / M % 2, j = i % M;
+            if constexpr (i < 2 * M) {
+                if (j & 1) dp[sb] = T::mfma(ring[i % AHEAD], vf[j / 2], dp[sb]);
+                else s[sb] = T::mfma(ring[i % AHEAD], kf[j / 2], s[sb]);
+            } else {
+                constexpr int kc = j / (2 * NB), d = j / 2 % NB;
+                if (j & 1) dk[d] = T::mfma(ring[i % AHEAD], dr[sb][kc], dk[d]);
+                else dv[d] = T::mfma(ring[i % AHEAD], pr[sb][kc], dv[d]);
+            }
+            if constexpr (i + AHEAD < 4 * M) ring[i % AHEAD] = operand(std::integral_constant<int, i + AHEAD>{});
+            if constexpr (i >= M && i < 3 * M) {
+                constexpr int h = i / M - 1;
+                static_for<j * 16 / M, (j + 1) * 16 / M>([&](auto nth) __attribute__((always_inline)) {
+                    constexpr int n = nth, four = 4 * h + n / 4;
+                    if constexpr (n % 4 == 0 && four < 7) row_stats(four + 1);
+                    element(d0 - (float)(32 * h + 8 * (n / 4) + n % 4), slope2, s[h][n], dp[h][n], lse2[four % 2][n % 4],
+                            delta[four % 2][n % 4], p[n % 2], ds[n % 2]);
+                    if constexpr (n % 2 == 1) {
+                        put_two<T>(pr[h][n / 8], n % 8 - 1, p);
+                        put_two<T>(dr[h][n / 8], n % 8 - 1, ds);
+                    }
+                });
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+
+    // All steps of a kind; the next one's rows are on their way meanwhile.
+    auto walk = [&](int kind, auto work) __attribute__((always_inline)) {
+        Step st = next(step_at(i0), kind);
+        if (st.i < i1) {
+            load(st, 0);
+            store(0);
+        }
         moved();
+        ready();
         __syncthreads();
-        i = i2;
+        for (int buf = 0; st.i < i1; buf ^= 1) {
+            const Step st2 = next(after(st), kind);
+            if (st2.i < i1) load(st2, buf ^ 1);
+            work(st, buf);
+            if (st2.i < i1) store(buf ^ 1);
+            moved();
+            __syncthreads();
+            st = st2;
+        }
+    };
+    if constexpr (NB == 2) {
+        walk(2, any_step);
+    } else {
+        // in loops of their own, or the sums would move between registers in every step
+        walk(0, any_step);
+        walk(1, whole);
     }
     if (key >= a.k_len) return;
     const int64_t units = (int64_t)a.batch * a.k_heads;
@@ -1085,7 +1200,11 @@ template <typename T, int NB, bool SHAPED> hipError_t backward_sized(const AttnA
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (a.k_len) {
-        dkv_kernel<T, NB, SHAPED><<<(unsigned)(units * ((a.k_len + GRAD_KEYS - 1) / GRAD_KEYS) * a.parts), 256, 0, st>>>(a);
+        const unsigned n = (unsigned)(units * ((a.k_len + GRAD_KEYS - 1) / GRAD_KEYS) * a.parts);
+        if (!SHAPED) dkv_kernel<T, NB, false, false><<<n, 256, 0, st>>>(a);
+        else if (!a.slopes) dkv_kernel<T, NB, true, false><<<n, 256, 0, st>>>(a);
+        else if (a.cap > 0) dkv_kernel<T, NB, true, true><<<n, 256, 0, st>>>(a);
+        else dkv_kernel<T, NB, false, true><<<n, 256, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
         if (a.parts > 1) grad_join_kernel<T><<<dim3((unsigned)((units * a.k_len + 7) / 8), 2), 256, 0, st>>>(a);
     }
