@@ -202,13 +202,24 @@ __device__ __forceinline__ const char *head_base(const Heads &t, int b, int head
     return t.data + (b * t.batch + head * t.head) * 2;
 }
 
-// Workgroups go round the 8 dies; neighbours in `unit` share keys, so each die
-// gets a contiguous range.
-__device__ __forceinline__ int spread(int id, int n)
-{
-    const int per = n / 8, rest = n % 8, x = id % 8, i = id / 8;
-    return x * per + min(x, rest) + i;
-}
+// The work of workgroup `id` of units x tiles: tiles of rank 0 (the longest
+// under a causal mask) first, so that the short ones fill the end.  Workgroups
+// go round the 8 dies; where the units divide among them, a die has units of
+// its own, whose keys its cache then holds.
+struct Work {
+    int unit, rank;
+    __device__ Work(int id, int units)
+    {
+        if (units % 8 == 0) {
+            const int each = units / 8, i = id / 8;
+            unit = id % 8 * each + i % each;
+            rank = i / each;
+        } else {
+            unit = id % units;
+            rank = id / units;
+        }
+    }
+};
 
 __global__ void __launch_bounds__(64) doc_tiles_kernel(AttnArgs a)
 {
@@ -386,12 +397,10 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
 
     const int row_tiles = (a.rows + ROW_TILE - 1) / ROW_TILE;
     const int units = a.batch * a.k_heads;
-    int id = spread(blockIdx.x, gridDim.x);
-    const int split = id % a.splits;
-    id /= a.splits;
-    // the longest first under a causal mask
-    const int tile_row = (row_tiles - 1 - id % row_tiles) * ROW_TILE;
-    RowBlock<ROW_TILE, 256> w(a, id / row_tiles, tile_row, tile_row + threadIdx.x / WAVE * 32 + threadIdx.x % 32, range);
+    const int split = blockIdx.x / (units * row_tiles);
+    const Work work(blockIdx.x % (units * row_tiles), units);
+    const int tile_row = (row_tiles - 1 - work.rank) * ROW_TILE;
+    RowBlock<ROW_TILE, 256> w(a, work.unit, tile_row, tile_row + threadIdx.x / WAVE * 32 + threadIdx.x % 32, range);
     if (a.splits > 1) {                                  // this part's tiles
         const int n = max(w.t1 - w.t0, 0), per = (n + a.splits - 1) / a.splits;
         w.t0 = min(w.t0, w.t1) + per * split;
@@ -544,9 +553,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
     __shared__ int range[4];
 
     const int units = a.batch * a.k_heads;
-    int id = spread(blockIdx.x, gridDim.x);
-    const int split = id % a.splits;
-    id /= a.splits;
+    const int id = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
     const int lane = threadIdx.x % WAVE, hi = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const RowBlock<FEW_ROWS, FEW_WAVES * WAVE> w(a, id, 0, lane % 32, range);
     const Unit &u = w.u;
@@ -778,9 +785,9 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
     __shared__ int range[4];
 
     const int row_tiles = (a.rows + ROW_TILE - 1) / ROW_TILE;
-    const int id = spread(blockIdx.x, gridDim.x);
-    const int tile_row = (row_tiles - 1 - id % row_tiles) * ROW_TILE;
-    const RowBlock<ROW_TILE, 256> w(a, id / row_tiles, tile_row, tile_row + threadIdx.x / WAVE * 32 + threadIdx.x % 32, range);
+    const Work work(blockIdx.x, a.batch * a.k_heads);
+    const int tile_row = (row_tiles - 1 - work.rank) * ROW_TILE;
+    const RowBlock<ROW_TILE, 256> w(a, work.unit, tile_row, tile_row + threadIdx.x / WAVE * 32 + threadIdx.x % 32, range);
     const Unit &u = w.u;
     const int lane = threadIdx.x % WAVE, hi = lane / 32;
 
@@ -888,12 +895,10 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
     __shared__ __align__(16) float lse2s[2][ROWS], deltas[2][ROWS];
     __shared__ __align__(16) int docs[2][ROWS];
 
-    const int key_blocks = (a.k_len + GRAD_KEYS - 1) / GRAD_KEYS;
-    int id = spread(blockIdx.x, gridDim.x);
-    const int part = id % a.parts;
-    id /= a.parts;
-    const Unit u(a, id / key_blocks);
-    const int j0 = id % key_blocks * GRAD_KEYS;
+    const int part = blockIdx.x % a.parts;
+    const Work work(blockIdx.x / a.parts, a.batch * a.k_heads);
+    const Unit u(a, work.unit);
+    const int j0 = work.rank * GRAD_KEYS;
     const int lane = threadIdx.x % WAVE, hi = lane / 32;
     const int jw = j0 + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) * 32, key = jw + lane % 32;
 
