@@ -78,6 +78,8 @@ template <int READS, int TIMES, int EACH, int VALUS> __device__ __forceinline__ 
     }
 }
 
+template <typename T> __device__ __forceinline__ float value_of(short bits) { return (float)__builtin_bit_cast(typename T::raw, bits); }
+
 // two numbers rounded into an operand's elements i and i + 1
 template <typename T> __device__ __forceinline__ void put_two(s16x8 &v, int i, const float (&x)[2])
 {
@@ -346,8 +348,12 @@ template <int ROWS, int THREADS> struct RowBlock {
         for (int i = 0; i < N; i++) x[i] = key0 + 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4 < end ? x[i] : other;
         if (!u.docs) return;
 #pragma unroll
-        for (int i = 0; i < N; i++)
-            x[i] = u.docs[min(key0 + 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4, a.k_len - 1)] == doc ? x[i] : other;
+        for (int i = 0; i < N; i += 4) {
+#pragma unroll
+            for (int n = 0; n < 4; n++)
+                x[i + n] = u.docs[min(key0 + 32 * (i / 16) + 8 * (i % 16 / 4) + n, a.k_len - 1)] == doc ? x[i + n] : other;
+            __builtin_amdgcn_sched_barrier(0);            // registers for four loads, not for all
+        }
     }
 };
 
@@ -746,37 +752,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
 // of all heads of the group.  Seven products instead of five, but every sum
 // has one owner and a fixed order: no atomics, the same bits each time.
 
-// log2-sum-exp2 (plus infinity for a row that sees nothing, so that its P is 0) and D
-template <typename T>
-__global__ void __launch_bounds__(256) row_stat_kernel(AttnArgs a)
-{
-    using R = typename T::raw;
-    typedef R r8 __attribute__((ext_vector_type(8)));
-    const int64_t n = (int64_t)a.batch * a.k_heads * a.rows;
-    const int64_t r = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    if (r >= n) return;
-    const int64_t unit = r / a.rows;
-    const int row = (int)(r % a.rows), b = (int)(unit / a.k_heads), g = (int)(unit % a.k_heads);
-    const int query = row / a.group, head = g * a.group + row % a.group, c = threadIdx.x % 16 * 8;
-    float sum = 0;
-    if (c < a.head_dim) {
-        const r8 x = *(const r8 *)(head_base(a.out, b, head) + (query * a.out.position + c) * 2);
-        const r8 y = *(const r8 *)(head_base(a.dout, b, head) + (query * a.dout.position + c) * 2);
-        r8 z = {};
-        if (a.rest) z = *(const r8 *)(a.rest + (((int64_t)b * a.q_len + query) * a.k_heads * a.group + head) * a.head_dim * 2 + c * 2);
-#pragma unroll
-        for (int i = 0; i < 8; i++) sum += ((float)x[i] + (float)z[i]) * (float)y[i];
-    }
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d);
-    if (c == 0) {
-        const int64_t at = ((int64_t)b * a.k_heads * a.group + head) * a.q_len + query;
-        const float lse = a.lse[at];
-        a.row_stat[at] = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, sum);
-    }
-}
-
-template <typename T, int NB, bool SHAPED>
+template <typename T, int NB, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
@@ -792,20 +768,32 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
     const int lane = threadIdx.x % WAVE, hi = lane / 32;
 
     s16x8 q[2 * NB], g[2 * NB];
+    float delta = 0;
     {
         const char *qp = head_base(a.q, u.b, w.head) + w.query * a.q.position * 2;
         const char *gp = head_base(a.dout, u.b, w.head) + w.query * a.dout.position * 2;
+        const char *op = head_base(a.out, u.b, w.head) + w.query * a.out.position * 2;
+        const char *rp = a.rest + (((int64_t)u.b * a.q_len + w.query) * a.k_heads * a.group + w.head) * a.head_dim * 2;
 #pragma unroll
         for (int s = 0; s < 2 * NB; s++) {
             const int d = 16 * s + 8 * hi;
-            q[s] = d < a.head_dim ? *(const s16x8 *)(qp + d * 2) : s16x8{};
-            g[s] = d < a.head_dim ? *(const s16x8 *)(gp + d * 2) : s16x8{};
+            const bool in = d < a.head_dim;
+            q[s] = in ? *(const s16x8 *)(qp + d * 2) : s16x8{};
+            g[s] = in ? *(const s16x8 *)(gp + d * 2) : s16x8{};
+            const s16x8 o = in ? *(const s16x8 *)(op + d * 2) : s16x8{}, r = in && a.rest ? *(const s16x8 *)(rp + d * 2) : s16x8{};
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                delta += (value_of<T>(o[i]) + value_of<T>(r[i])) * value_of<T>(g[s][i]);
         }
+        delta += other_half(delta);
     }
-    const float2 stat = a.row_stat[((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query];
-    const bool capped = a.cap > 0, bias = a.slopes != nullptr;
-    const float slope2 = bias ? a.slopes[w.head] * LOG2E : 0.0f;
-    const float scale2 = capped ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    // log2-sum-exp2 (plus infinity for a row that sees nothing, so that its P
+    // is 0) and D, for the kernel of dK and dV too
+    const int64_t stat_at = ((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query;
+    const float lse = a.lse[stat_at], lse2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
+    if (hi == 0 && w.row < a.rows) a.row_stat[stat_at] = make_float2(lse2, delta);
+    const float slope2 = BIAS ? a.slopes[w.head] * LOG2E : 0.0f;
+    const float scale2 = CAP ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
     f32x16 dq[NB] = {};
     const char *kb = head_base(a.k, u.b, u.g), *vb = head_base(a.v, u.b, u.g);
 
@@ -825,47 +813,55 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
             mv.load(tiles + (2 + (buf ^ 1)) * SIZE, vb, t2 * KEY_TILE, u.len, a.head_dim);
         }
         if (j0 < w.wave_end) {
-            short *ks = tiles + buf * SIZE;
-            const short *vs = tiles + (2 + buf) * SIZE;
+            short *const ks = tiles + buf * SIZE, *const vs = tiles + (2 + buf) * SIZE;
             const bool whole = w.whole(t);
-#pragma unroll
-            for (int kb2 = 0; kb2 < 2; kb2++) {
+            // The matrix instructions of both halves of the tile in order: scores
+            // and dP, then dQ; operands are read from LDS four ahead.
+            constexpr int M1 = 4 * NB, M = M1 + 2 * NB, AHEAD = 4;
+            s16x8 ring[AHEAD];
+            auto operand = [&](auto at) __attribute__((always_inline)) {
+                constexpr int i = at, half = i / M, j = i % M;
+                if constexpr (j < M1) return L::row_operand(j & 1 ? vs : ks, 32 * half + lane % 32, j / 2);
+                else return L::column_operand(ks, 32 * half + 16 * ((j - M1) / NB), (j - M1) % NB);
+            };
+            auto ahead = [&](auto at) __attribute__((always_inline)) {
+                if constexpr (at + AHEAD < 2 * M) ring[at % AHEAD] = operand(std::integral_constant<int, at + AHEAD>{});
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            static_for<0, AHEAD>([&](auto at) __attribute__((always_inline)) { ring[at] = operand(at); });
+            static_for<0, 2>([&](auto nth) __attribute__((always_inline)) {
+                constexpr int half = nth;
                 f32x16 s = {}, dp = {};
+                static_for<half * M, half * M + M1>([&](auto at) __attribute__((always_inline)) {
+                    constexpr int j = at % M;
+                    if constexpr (j & 1) dp = T::mfma(ring[at % AHEAD], g[j / 2], dp);
+                    else s = T::mfma(ring[at % AHEAD], q[j / 2], s);
+                    ahead(at);
+                });
+                float x[16];
+                const float pf = (float)(w.pos - j0 - 32 * half - 4 * hi);
 #pragma unroll
-                for (int st = 0; st < 2 * NB; st++) {
-                    s = T::mfma(L::row_operand(ks, 32 * kb2 + lane % 32, st), q[st], s);
-                    dp = T::mfma(L::row_operand(vs, 32 * kb2 + lane % 32, st), g[st], dp);
-                }
-                float x[16], y[16];
-                if (SHAPED && capped) {
-#pragma unroll
-                    for (int i = 0; i < 16; i++) {
+                for (int i = 0; i < 16; i++) {
+                    float y;
+                    x[i] = dp[i] - delta;
+                    if (CAP) {
                         const float th = tanh_of(s[i] * scale2);
-                        y[i] = fmaf(cap2, th, -stat.x);
-                        x[i] = (dp[i] - stat.y) * fmaf(-th, th, 1.0f);
+                        y = fmaf(cap2, th, -lse2);
+                        x[i] *= fmaf(-th, th, 1.0f);
+                    } else {
+                        y = fmaf(s[i], scale2, -lse2);
                     }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        y[i] = fmaf(s[i], scale2, -stat.x);
-                        x[i] = dp[i] - stat.y;
-                    }
+                    if (BIAS) y -= slope2 * fabsf(pf - (float)(8 * (i / 4) + i % 4));
+                    x[i] *= exp2_(y);
                 }
-                if (SHAPED && bias) {
-                    const float pf = (float)(w.pos - j0 - 32 * kb2 - 4 * hi);
-#pragma unroll
-                    for (int i = 0; i < 16; i++) y[i] -= slope2 * fabsf(pf - (float)(8 * (i / 4) + i % 4));
-                }
-#pragma unroll
-                for (int i = 0; i < 16; i++) x[i] *= exp2_(y[i]);
-                if (!whole) w.mask(a, x, j0 + 32 * kb2 + 4 * hi, 0.0f);
-#pragma unroll
-                for (int kc = 0; kc < 2; kc++) {
-                    const s16x8 p = rounded<T>(x + 8 * kc);
-#pragma unroll
-                    for (int d = 0; d < NB; d++) dq[d] = T::mfma(L::column_operand(ks, 32 * kb2 + 16 * kc, d), p, dq[d]);
-                }
-            }
+                if (!whole) w.mask(a, x, j0 + 32 * half + 4 * hi, 0.0f);
+                const s16x8 p[2] = {rounded<T>(x), rounded<T>(x + 8)};
+                static_for<half * M + M1, half * M + M>([&](auto at) __attribute__((always_inline)) {
+                    constexpr int j = at % M - M1;
+                    dq[j % NB] = T::mfma(ring[at % AHEAD], p[j / NB], dq[j % NB]);
+                    ahead(at);
+                });
+            });
         }
         moved();
         __syncthreads();
@@ -1195,25 +1191,25 @@ template <typename T, int NB, bool SHAPED> hipError_t forward_sized(const AttnAr
     return hipGetLastError();
 }
 
-template <typename T, int NB, bool SHAPED> hipError_t backward_sized(const AttnArgs &a, hipStream_t st)
+template <typename T, int NB, bool CAP, bool BIAS> hipError_t backward_shaped(const AttnArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
     if (a.rows) {
-        row_stat_kernel<T><<<(unsigned)((units * a.rows + 15) / 16), 256, 0, st>>>(a);
-        if (hipError_t e = hipGetLastError()) return e;
-        dq_kernel<T, NB, SHAPED><<<(unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE)), 256, 0, st>>>(a);
+        dq_kernel<T, NB, CAP, BIAS><<<(unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE)), 256, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (a.k_len) {
-        const unsigned n = (unsigned)(units * ((a.k_len + GRAD_KEYS - 1) / GRAD_KEYS) * a.parts);
-        if (!SHAPED) dkv_kernel<T, NB, false, false><<<n, 256, 0, st>>>(a);
-        else if (!a.slopes) dkv_kernel<T, NB, true, false><<<n, 256, 0, st>>>(a);
-        else if (a.cap > 0) dkv_kernel<T, NB, true, true><<<n, 256, 0, st>>>(a);
-        else dkv_kernel<T, NB, false, true><<<n, 256, 0, st>>>(a);
+        dkv_kernel<T, NB, CAP, BIAS><<<(unsigned)(units * ((a.k_len + GRAD_KEYS - 1) / GRAD_KEYS) * a.parts), 256, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
         if (a.parts > 1) grad_join_kernel<T><<<dim3((unsigned)((units * a.k_len + 7) / 8), 2), 256, 0, st>>>(a);
     }
     return hipGetLastError();
+}
+
+template <typename T, int NB> hipError_t backward_sized(const AttnArgs &a, hipStream_t st)
+{
+    if (a.cap > 0) return a.slopes ? backward_shaped<T, NB, true, true>(a, st) : backward_shaped<T, NB, true, false>(a, st);
+    return a.slopes ? backward_shaped<T, NB, false, true>(a, st) : backward_shaped<T, NB, false, false>(a, st);
 }
 
 template <typename T> hipError_t forward_typed(const AttnArgs &a, hipStream_t st)
@@ -1226,10 +1222,7 @@ template <typename T> hipError_t forward_typed(const AttnArgs &a, hipStream_t st
 
 template <typename T> hipError_t backward_typed(const AttnArgs &a, hipStream_t st)
 {
-    const bool shaped = a.cap > 0 || a.slopes;
-    if (a.head_dim <= 64) return shaped ? backward_sized<T, 2, true>(a, st) : backward_sized<T, 2, false>(a, st);
-    if (a.head_dim <= 96) return shaped ? backward_sized<T, 3, true>(a, st) : backward_sized<T, 3, false>(a, st);
-    return shaped ? backward_sized<T, 4, true>(a, st) : backward_sized<T, 4, false>(a, st);
+    return a.head_dim <= 64 ? backward_sized<T, 2>(a, st) : a.head_dim <= 96 ? backward_sized<T, 3>(a, st) : backward_sized<T, 4>(a, st);
 }
 
 }  // namespace
