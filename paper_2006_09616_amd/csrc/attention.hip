@@ -34,6 +34,7 @@ struct Bf16 {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
     static constexpr float p_gain = 1.0f, p_shift = 0.0f;
+    static constexpr uint32_t exponent = 0x7F807F80u, least = 0x00800080u;     // of two numbers, and its lowest bits
 };
 // Backward probabilities of long rows are below the smallest normal number
 // of fp16; 2^6 keeps six more bits of them (they are at most 1).
@@ -45,6 +46,7 @@ struct Fp16 {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
     static constexpr float p_gain = 64.0f, p_shift = 6.0f;
+    static constexpr uint32_t exponent = 0x7C007C00u, least = 0x04000400u;
 };
 
 // eight numbers rounded to the inputs' type: an operand of the next product
@@ -79,6 +81,50 @@ template <int READS, int TIMES, int EACH, int VALUS> __device__ __forceinline__ 
 }
 
 template <typename T> __device__ __forceinline__ float value_of(short bits) { return (float)__builtin_bit_cast(typename T::raw, bits); }
+
+// Infinities and NaN.  A matrix instruction multiplies them by the zero
+// probability of a masked pair, which gives NaN where the definition has
+// nothing.  So tiles that a mask cuts through (and only they) are searched for
+// them; they are replaced by zeros, and what visible values give is added to
+// the finished sums (add_nonfinite).
+template <typename T> __device__ __forceinline__ uint32_t nonfinite(uint32_t two)      // top bits of those of two
+{
+    return ((two & T::exponent) + T::least) & 0x80008000u;
+}
+template <typename T> __device__ __forceinline__ bool nonfinite(const uint4 &v)
+{
+    return nonfinite<T>(v.x) | nonfinite<T>(v.y) | nonfinite<T>(v.z) | nonfinite<T>(v.w);
+}
+template <typename T> __device__ __forceinline__ uint4 cleaned(uint4 v)
+{
+    v.x &= ~((nonfinite<T>(v.x) >> 15) * 0xFFFFu);
+    v.y &= ~((nonfinite<T>(v.y) >> 15) * 0xFFFFu);
+    v.z &= ~((nonfinite<T>(v.z) >> 15) * 0xFFFFu);
+    v.w &= ~((nonfinite<T>(v.w) >> 15) * 0xFFFFu);
+    return v;
+}
+// Tiles of SIZE elements, by all 256 threads (one tile: a and b the same).
+// Returns whether a and whether b had any.
+struct Odd { bool a, b; };
+template <typename T, int SIZE> __device__ Odd clean(short *a, short *b)
+{
+    constexpr int N = SIZE / 8 / 256;
+    uint4 *const p = (uint4 *)a + threadIdx.x, *const q = (uint4 *)b + threadIdx.x;
+    bool any_a = false, any_b = false;
+#pragma unroll 2
+    for (int n = 0; n < N; n++) {
+        any_a |= nonfinite<T>(p[n * 256]);
+        if (a != b) any_b |= nonfinite<T>(q[n * 256]);
+    }
+    if (!__syncthreads_or(any_a | any_b)) return {false, false};
+    if (any_a)
+#pragma unroll 1
+        for (int n = 0; n < N; n++) p[n * 256] = cleaned<T>(p[n * 256]);
+    if (any_b)
+#pragma unroll 1
+        for (int n = 0; n < N; n++) q[n * 256] = cleaned<T>(q[n * 256]);
+    return {(bool)__syncthreads_or(any_a), (bool)__syncthreads_or(any_b)};
+}
 
 // two numbers rounded into an operand's elements i and i + 1
 template <typename T> __device__ __forceinline__ void put_two(s16x8 &v, int i, const float (&x)[2])
@@ -250,6 +296,18 @@ __device__ __forceinline__ void write_four(const Heads &t, int b, int head, int6
     *(typename Four<R>::v *)(t.data + (b * t.batch + head * t.head + position * t.position + col) * 2) = r;
 }
 
+// adds to four columns of the output that the same lane has written
+template <typename T>
+__device__ __forceinline__ void add_out(const AttnArgs &a, int b, int head, int64_t query, int col, f32x4 v)
+{
+    using R = typename T::raw;
+    auto *p = (typename Four<R>::v *)(a.out.data + (b * a.out.batch + head * a.out.head + query * a.out.position + col) * 2);
+    typename Four<R>::v r = *p;
+#pragma unroll
+    for (int i = 0; i < 4; i++) r[i] = (R)((float)r[i] + v[i]);
+    *p = r;
+}
+
 // Four columns of the output and, for the backward pass, what the rounding
 // took from them: out . dout is subtracted from every score gradient of its
 // row, so that its error does not average out over the keys.
@@ -331,15 +389,19 @@ template <int ROWS, int THREADS> struct RowBlock {
             while (t < t1 && !near(t)) t++;
         return t;
     }
-    // whether every row sees every key of the tile
-    __device__ bool whole(int t) const
+    __device__ bool same_doc(int t) const
     {
-        bool w = (t + 1) * KEY_TILE <= sure;
-        if (u.docs) {
-            const int2 d = u.doc_tiles[t];
-            w = w && one_doc && d.x == d.y;
-        }
-        return w;
+        if (!u.docs) return true;
+        const int2 d = u.doc_tiles[t];
+        return one_doc && d.x == d.y;
+    }
+    // whether every row sees every key of the tile
+    __device__ bool whole(int t) const { return (t + 1) * KEY_TILE <= sure && same_doc(t); }
+    // whether some row does not see a key that is there (from u.len on there are zeros)
+    __device__ bool cut(int t) const { return min((t + 1) * KEY_TILE, u.len) > sure || !same_doc(t); }
+    __device__ bool sees(const AttnArgs &a, int key) const
+    {
+        return key < end && (!u.docs || u.docs[min(key, a.k_len - 1)] == doc);
     }
     // x = other for the lane's keys (key0 + 32 (i / 16) + 8 (i % 16 / 4) + i % 4) that its row does not see
     template <int N> __device__ void mask(const AttnArgs &a, float (&x)[N], int key0, float other) const
@@ -356,6 +418,27 @@ template <int ROWS, int THREADS> struct RowBlock {
         }
     }
 };
+
+// What the infinities and NaN of the values of keys j0 .. j1 - 1 add to four
+// columns of a row that sees those keys: a positive probability of them is
+// them.  Rarely called: for tiles that had any.
+template <typename T, typename Sees>
+__device__ __forceinline__ void add_nonfinite(const AttnArgs &a, const char *vb, int j0, int j1, int col, Sees sees, f32x4 &sum)
+{
+#pragma unroll 1
+    for (int j = j0; j < j1; j++) {
+        const s16x4 v = *(const s16x4 *)(vb + j * a.v.position * 2 + col * 2);
+        bool any = false;
+        f32x4 f;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            f[i] = value_of<T>(v[i]);
+            if (fabsf(f[i]) < INFINITY) f[i] = 0.0f;
+            else any = true;
+        }
+        if (any && sees(j)) sum += f;
+    }
+}
 
 // The scores of a lane's keys (key0 + 4 (lane / 32) + 32 (i / 16) + 8 (i % 16 / 4)
 // + i % 4), shaped in place: times log2(e), capped, biased.
@@ -428,6 +511,7 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
 
     f32x16 o[NB] = {};
     float m = LOWEST, l = 0;
+    bool odd = false;                                    // whether cleaned values are to be added
     const char *kb = head_base(a.k, u.b, u.g), *vb = head_base(a.v, u.b, u.g);
 
     int t = w.next(w.t0);
@@ -445,9 +529,11 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
             mk.load(tiles + (buf ^ 1) * SIZE, kb, t2 * KEY_TILE, u.len, a.head_dim);
             mv.load(tiles + (2 + (buf ^ 1)) * SIZE, vb, t2 * KEY_TILE, u.len, a.head_dim);
         }
+        const bool whole = w.whole(t);
+        short *const vs = tiles + (2 + buf) * SIZE;
+        if (w.cut(t)) odd |= clean<T, SIZE>(vs, vs).a;
         if (j0 < w.wave_end) {
             const short *ks = tiles + buf * SIZE;
-            short *vs = tiles + (2 + buf) * SIZE;
             // operands are read from LDS a group of products ahead
             f32x16 s[2] = {};
             s16x8 f[2][4];
@@ -475,7 +561,7 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
 #pragma unroll
             for (int i = 0; i < 32; i++) x[i] = s[i / 16][i % 16];
             if (SHAPED) shape.apply(x, w.pos - j0 - 4 * hi);
-            if (!w.whole(t)) w.mask(a, x, j0 + 4 * hi, -INFINITY);
+            if (!whole) w.mask(a, x, j0 + 4 * hi, -INFINITY);
             float most = x[0];
 #pragma unroll
             for (int i = 1; i < 32; i++) most = fmaxf(most, x[i]);
@@ -510,31 +596,37 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
     l += other_half(l);
     if (w.row >= a.rows) return;
     const bool nothing = l == 0;
-    if (a.splits > 1) {
-        const int64_t at = ((int64_t)split * units + u.b * a.k_heads + u.g) * a.rows + w.row;
-        float *po = a.part_out + at * a.head_dim;
-#pragma unroll
-        for (int d = 0; d < NB; d++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const int col = 32 * d + 8 * e + 4 * hi;
-                if (col < a.head_dim) *(f32x4 *)(po + col) = f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
-            }
-        if (hi == 0) a.part_stat[at] = make_float2(m, l);
-        return;
-    }
     const float inv = nothing ? 0.0f : 1.0f / l;
+    const int64_t part_at = ((int64_t)split * units + u.b * a.k_heads + u.g) * a.rows + w.row;
+    auto write = [&](int col, f32x4 v) {
+        if (a.splits > 1) *(f32x4 *)(a.part_out + part_at * a.head_dim + col) = v;
+        else write_out<T>(a, u.b, w.head, w.query, col, nothing ? f32x4{} : v * inv);
+    };
 #pragma unroll
     for (int d = 0; d < NB; d++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int col = 32 * d + 8 * e + 4 * hi;
-            f32x4 v = {o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
-            if (col < a.head_dim) write_out<T>(a, u.b, w.head, w.query, col, nothing ? f32x4{} : v * inv);
+            if (col < a.head_dim) write(col, f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]});
         }
-    if (a.lse && hi == 0)
-        a.lse[((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query] =
-            nothing ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    if (hi == 0) {
+        if (a.splits > 1) a.part_stat[part_at] = make_float2(m, l);
+        else if (a.lse)
+            a.lse[((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query] =
+                nothing ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    }
+    if (!odd) return;
+    for (int col = 4 * hi; col < a.head_dim; col += 8) {
+        f32x4 sum = {};
+        for (int t = w.next(w.t0); t < w.t1; t = w.next(t + 1))
+            if (w.cut(t))
+                add_nonfinite<T>(a, vb, t * KEY_TILE, min((t + 1) * KEY_TILE, u.len), col, [&](int j) { return w.sees(a, j); }, sum);
+        // finite columns have been written; an infinity or NaN takes its column whole
+        const bool any = !(fabsf(sum[0]) + fabsf(sum[1]) + fabsf(sum[2]) + fabsf(sum[3]) < INFINITY);
+        if (!any) continue;
+        if (a.splits > 1) *(f32x4 *)(a.part_out + part_at * a.head_dim + col) += sum;
+        else add_out<T>(a, u.b, w.head, w.query, col, sum);
+    }
 }
 
 // Few rows (at most 32 of a key head: new tokens over a cache): what bounds it
@@ -584,6 +676,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
     const Shape shape(a, w.head);
     f32x16 o[NB] = {};
     float m = LOWEST, l = 0;
+    bool odd = false;                                    // whether cleaned values are to be added
     const char *kb = head_base(a.k, u.b, u.g), *vb = head_base(a.v, u.b, u.g);
     short *vt = (short *)lds + wave * SIZE;
     const uint32_t koff = (uint32_t)(lane % 32 * (uint32_t)a.k.position + 8 * hi) * 2u;
@@ -618,6 +711,17 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
     if (t < t1) load(t);
     while (t < t1) {
         const int j0 = t * FEW_KEYS, t2 = next(t + FEW_WAVES);
+        const bool masked = j0 + FEW_KEYS > w.sure || u.docs;
+        if (min(j0 + FEW_KEYS, u.len) > w.sure || u.docs) {
+            bool any = false;
+#pragma unroll
+            for (int n = 0; n < N; n++) any |= nonfinite<T>(vr[n]);
+            if (__any(any)) {
+                odd = true;
+#pragma unroll
+                for (int n = 0; n < N; n++) vr[n] = cleaned<T>(vr[n]);
+            }
+        }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int n = 0; n < N; n++) *(uint4 *)(vt + L::at(vrow + n * STEP, vchunk)) = vr[n];
@@ -630,7 +734,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
 #pragma unroll
         for (int i = 0; i < 16; i++) x[i] = s[i];
         if (SHAPED) shape.apply(x, w.pos - j0 - 4 * hi);
-        if (j0 + FEW_KEYS > w.sure || u.docs) w.mask(a, x, j0 + 4 * hi, -INFINITY);
+        if (masked) w.mask(a, x, j0 + 4 * hi, -INFINITY);
         float most = x[0];
 #pragma unroll
         for (int i = 1; i < 16; i++) most = fmaxf(most, x[i]);
@@ -672,7 +776,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
                     f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
         if (hi == 0) stats[wave][lane] = make_float2(m, l);
     }
-    __syncthreads();
+    odd = __syncthreads_or(odd);
     for (int i = threadIdx.x; i < rows * COLS; i += FEW_WAVES * WAVE) {
         const int r = i / COLS, col = i % COLS * 4;
         float most = LOWEST, total = 0;
@@ -684,6 +788,14 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
             const float f = exp2_(stats[v][r].x - most);
             total += stats[v][r].y * f;
             sum += sums[v * rows * COLS + i] * f;
+        }
+        if (odd && col < a.head_dim) {
+            const int pos = u.start + r / a.group, end = u.end(a, pos);
+            const bool has_doc = !u.docs || (pos >= 0 && pos < a.k_len);
+            const int first = u.docs ? t0 : max(t0, w.sure / FEW_KEYS);           // the tiles that were cleaned
+            if (has_doc)
+                add_nonfinite<T>(a, vb, first * FEW_KEYS, min(t1 * FEW_KEYS, u.len), col,
+                                 [&](int j) { return j < end && (!u.docs || u.docs[j] == u.docs[pos]); }, sum);
         }
         if (a.splits > 1) {
             const int64_t at = ((int64_t)split * units + id) * a.rows + r;
@@ -812,12 +924,15 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
             mk.load(tiles + (buf ^ 1) * SIZE, kb, t2 * KEY_TILE, u.len, a.head_dim);
             mv.load(tiles + (2 + (buf ^ 1)) * SIZE, vb, t2 * KEY_TILE, u.len, a.head_dim);
         }
+        short *const ks = tiles + buf * SIZE, *const vs = tiles + (2 + buf) * SIZE;
+        const bool whole = w.whole(t);
+        // a row that sees one of them has it in its log-sum-exp or in out . dout
+        if (w.cut(t)) clean<T, SIZE>(ks, vs);
         if (j0 < w.wave_end) {
-            short *const ks = tiles + buf * SIZE, *const vs = tiles + (2 + buf) * SIZE;
-            const bool whole = w.whole(t);
             // The matrix instructions of both halves of the tile in order: scores
-            // and dP, then dQ; operands are read from LDS four ahead.
-            constexpr int M1 = 4 * NB, M = M1 + 2 * NB, AHEAD = 4;
+            // and dP, then dQ; operands are read from LDS four ahead (two where
+            // registers are short, which measured the same).
+            constexpr int M1 = 4 * NB, M = M1 + 2 * NB, AHEAD = NB == 4 ? 2 : 4;
             s16x8 ring[AHEAD];
             auto operand = [&](auto at) __attribute__((always_inline)) {
                 constexpr int i = at, half = i / M, j = i % M;
@@ -1010,6 +1125,12 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
     // A step, 32 queries after the other, whatever the masks.
     auto any_step = [&](const Step &st, int buf) {
         const bool in_doc = same_doc(st.q0);
+        bool odd = false;
+        if (!in_doc || min(j0 + GRAD_KEYS, u.len) > u.end(a, u.start + st.q0)) {
+            // of a query with one of them, log-sum-exp or out . dout has it, and so
+            // has what it adds to dK; to dV out . dout takes it (below)
+            odd = clean<T, SIZE>(tiles + buf * SIZE, tiles + (2 + buf) * SIZE).b;
+        }
         const float slope2 = BIAS ? a.slopes[u.g * a.group + st.head] * LOG2E : 0.0f;
 #pragma unroll 1
         for (int sb = 0; sb < 2; sb++) {
@@ -1032,6 +1153,12 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
                 for (int n = 0; n < 4; n++)
                     element(d0 - (float)(8 * e + n), slope2, s[4 * e + n], dp[4 * e + n], lse2[n], delta[n], p[4 * e + n], ds[4 * e + n]);
             }
+            if (odd)
+#pragma unroll
+                for (int n = 0; n < 16; n++) {
+                    const float delta = deltas[buf][32 * sb + 8 * (n / 4) + 4 * hi + n % 4];
+                    p[n] += delta - delta;                 // NaN where it is no number
+                }
             if (!in_doc || jw + 32 > u.end(a, pb)) {
                 // queries of the 32 that see the key: from `from` on
                 const int from = key >= u.len ? INT32_MAX : a.causal && key >= u.prefix ? key - pb - 4 * hi : INT32_MIN;
@@ -1144,8 +1271,9 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int col = 32 * d + 8 * e + 4 * hi;
-            const f32x4 x = f32x4{dk[d][4 * e], dk[d][4 * e + 1], dk[d][4 * e + 2], dk[d][4 * e + 3]} * a.scale;
-            const f32x4 y = f32x4{dv[d][4 * e], dv[d][4 * e + 1], dv[d][4 * e + 2], dv[d][4 * e + 3]} * (1.0f / T::p_gain);
+            f32x4 x = f32x4{dk[d][4 * e], dk[d][4 * e + 1], dk[d][4 * e + 2], dk[d][4 * e + 3]} * a.scale;
+            f32x4 y = f32x4{dv[d][4 * e], dv[d][4 * e + 1], dv[d][4 * e + 2], dv[d][4 * e + 3]} * (1.0f / T::p_gain);
+            if (key >= u.len) x = y = f32x4{};            // whatever the queries hold
             if (col >= a.head_dim) continue;
             if (a.parts > 1) {
                 *(f32x4 *)(part_k + col) = x;

@@ -269,6 +269,90 @@ def test_attention_nothing_beyond_the_length(ops):
     check(ops, q, k, v, do, "padding, split", lengths=lengths, backward=False)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Sq,Sk", [(150, 150), (20, 150), (7, 150), (150, 1300)])
+def test_attention_infinities_and_nan_of_other_queries(ops, dtype, D, Sq, Sk):
+    """Keys and values that are not numbers reach the queries that see them,
+    and no others, also where both are worked on together."""
+    q, k, v, do = inputs(1, Sq, Sk, 2, 1, D, dtype)
+    a, b, c = Sk - Sq // 3 * 2, Sk - Sq // 3 - 1, Sk - 1  # seen by about two thirds, one third and one of the queries
+    want, tol = definition(q, k, v, do, D ** -0.5, 0.0, None, True, None, None, None, None)
+    clean = v.detach().clone()
+    clean[0, a, 0, 3] = clean[0, b, 0, 5] = 0             # only these columns change
+    want, tol = definition(q, k, clean, do, D ** -0.5, 0.0, None, True, None, None, None, None)
+    v.data[0, a, 0, 3] = float("nan")
+    v.data[0, b, 0, 5] = float("-inf")
+    k.data[0, c] = float("nan")
+    out = ops.attention(q, k, v, causal=True)
+    with torch.no_grad():
+        assert torch.equal(ops.attention(q, k, v, causal=True).nan_to_num(7, 8, 9), out.detach().nan_to_num(7, 8, 9))
+    got = out.detach().cpu().double()
+    pos = torch.arange(Sq) + Sk - Sq
+    assert torch.isnan(got[0, pos >= c]).all()
+    assert torch.isnan(got[0, pos >= a][:, :, 3]).all()
+    assert (got[0, (pos >= b) & (pos < c)][:, :, 5] == -math.inf).all()
+    ok = torch.ones_like(got, dtype=torch.bool)
+    ok[0, pos >= c] = False
+    ok[0, pos >= a, :, 3] = False
+    ok[0, pos >= b, :, 5] = False
+    assert torch.isfinite(got[ok]).all()
+    assert ((got - want["out"]).abs() <= tol["out"])[ok].all()
+    dq, = torch.autograd.grad(out, q, do)
+    rows = pos < a
+    assert ((dq.cpu().double() - want["dq"]).abs() <= tol["dq"])[0, rows].all()
+    assert torch.isnan(dq[0, (pos >= a).cuda()]).any(-1).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [64, 96, 128])
+def test_attention_a_document_of_nan(ops, dtype, D):
+    """A document of nothing but NaN leaves the others' outputs and gradients alone."""
+    S = 200
+    docs = torch.zeros(1, S, dtype=torch.int32)
+    docs[0, 40:75] = 1
+    docs[0, 130:190:2] = 1
+    bad = (docs[0] == 1)
+    for causal in (False, True):
+        q, k, v, do = inputs(1, S, S, 4, 2, D, dtype)
+        kw = dict(scale=D ** -0.5, cap=0.0, slopes=None, causal=causal, prefix=None, docs=docs, lengths=None, starts=None)
+        want, tol = definition(q, k, v, do, *kw.values())
+        for t in (q, k, v, do):
+            t.data[:, bad.cuda()] = float("nan")
+        out = ops.attention(q, k, v, causal=causal, docs=docs.cuda())
+        grads = torch.autograd.grad(out, (q, k, v), do)
+        for n, t in zip(("out", "dq", "dk", "dv"), (out.detach(), *grads)):
+            t = t.cpu().double()
+            assert torch.isnan(t[:, bad]).all(), n
+            close(t[:, ~bad], want[n][:, ~bad], tol[n][:, ~bad], f"{n} causal {causal}")
+
+
+def test_attention_gradient_alone_is_not_a_number(ops):
+    """A NaN in the output's gradient of one query reaches the values and keys that it sees only."""
+    q, k, v, do = inputs(1, 160, 160, 2, 2, 64, BF)
+    want, tol = definition(q, k, v, torch.cat([do[:, :70], torch.zeros_like(do[:, 70:71]), do[:, 71:]], 1), 0.125, 0.0, None,
+                           True, None, None, None, None)
+    do.data[:, 70] = float("nan")
+    dq, dk, dv = torch.autograd.grad(ops.attention(q, k, v, causal=True), (q, k, v), do)
+    assert torch.isnan(dv[:, :71]).all() and torch.isnan(dk[:, :71]).all() and torch.isnan(dq[:, 70]).all()
+    close(dv[:, 71:], want["dv"][:, 71:], tol["dv"][:, 71:], "dv")
+    close(dk[:, 71:], want["dk"][:, 71:], tol["dk"][:, 71:], "dk")
+    keep = torch.arange(160) != 70
+    close(dq[:, keep.cuda()], want["dq"][:, keep], tol["dq"][:, keep], "dq")
+
+
+def test_attention_lengths_out_of_range(ops):
+    """Lengths beyond the key slots count as all of them, negative ones as none."""
+    q, k, v, do = inputs(2, 20, 90, 2, 1, 64, FP)
+    with torch.no_grad():
+        for bad, good in (([1000, -7], [90, 0]), ([2 ** 31 - 1, -2 ** 31], [90, 0])):
+            a = ops.attention(q, k, v, lengths=torch.tensor(bad, dtype=torch.int64).cuda())
+            b = ops.attention(q, k, v, lengths=torch.tensor(good, dtype=torch.int32).cuda())
+            assert torch.equal(a, b)
+        far = ops.attention(q, k, v, causal=True, starts=torch.tensor([2 ** 40, -2 ** 40]).cuda())
+        assert torch.equal(far[0], ops.attention(q, k, v)[0]) and not far[1].any()
+
+
 def test_attention_empty(ops):
     dev = "cuda"
     for B, Sq, Sk in ((0, 4, 4), (2, 0, 5), (2, 5, 0), (1, 0, 0)):
