@@ -46,7 +46,7 @@ struct LogpArgs {
     const int64_t *tokens;
     float *logp, *entropy, *lse, *top_logp;
     int64_t *top_ids;
-    float *part;                  // [rows][splits][4] maximum, sum, weighted sum
+    float *part;                  // [rows][splits][4] maximum, sum, weighted sum, the token's logit
     float2 *part_top;             // [rows][splits][top] value, column (as bits)
 };
 

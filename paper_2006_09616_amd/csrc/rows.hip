@@ -378,22 +378,23 @@ __device__ Top segment_top(const Segment<T, WAVES> &g, int k)
 }
 
 // A workgroup's alternatives among its part of a row.  The statistics' pass
-// has left each lane the maximum of its own columns: the k-th largest of these
-// 256 bounds the part's k-th largest element from below, and just the k lanes
-// that reach it (more where maxima are equal) own elements that do.  Their
-// columns are read again, and of the few elements found each counts how many
-// are ahead of it.  Where more are found than there is room for, as among many
-// equal ones, or fewer than k numbers, the wavefronts' lists do it instead.
+// has left each lane the maximum of its own columns: a wavefront's k-th
+// largest of these bounds the part's k-th largest element from below, and only
+// the lanes that reach the best of the four bounds (at most 4 k, more where
+// maxima are equal) own elements that do.  Their columns are read again, and
+// of the few elements found each counts how many are ahead of it.  Where more
+// are found than there is room for, as among many equal ones, or fewer than k
+// numbers, the wavefronts' lists do it instead.
 constexpr int FOUND = 512;
 
 struct TopScratch {
-    float most[256];
-    int lanes[256];
+    float bars[SEGS];
+    int lanes[256], kept[128];
+    float maxima[256];
     float2 found[FOUND];
     float2 lists[SEGS][32];
     float2 best[32];                     // the result: value, column (as bits; -1: none), largest first
-    int n_lanes, n_found;
-    float bar;
+    int n_lanes, n_kept, n_found;
 };
 
 template <typename T>
@@ -401,22 +402,24 @@ __device__ void part_top(TopScratch &w, const Segment<T, SEGS> &g, float most, i
 {
     constexpr int N = T::vec;
     const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE;
-    w.most[tid] = most;
-    if (tid == 0) w.n_lanes = w.n_found = 0;
-    if (tid < 32) w.best[tid] = make_float2(0, __int_as_float(-1));
-    __syncthreads();
+    // each wavefront's k-th largest lane; the largest of these bounds the row's
     int rank = 0;
 #pragma unroll 8
-    for (int j = 0; j < 256; j += 4) {
-        const float4 o = *(const float4 *)&w.most[j];
-        rank += (o.x > most || (o.x == most && j < tid)) + (o.y > most || (o.y == most && j + 1 < tid)) +
-                (o.z > most || (o.z == most && j + 2 < tid)) + (o.w > most || (o.w == most && j + 3 < tid));
+    for (int j = 0; j < WAVE; j++) {
+        const float o = lane_value(most, j);
+        rank += o > most || (o == most && j < lane);
     }
-    if (rank == k - 1) w.bar = most;
+    if (rank == k - 1) w.bars[wave] = most;
+    if (tid == 0) w.n_lanes = w.n_kept = w.n_found = 0;
+    if (tid < 32) w.best[tid] = make_float2(0, __int_as_float(-1));
     __syncthreads();
-    const float bar = w.bar;
-    if (most >= bar) w.lanes[atomicAdd(&w.n_lanes, 1)] = tid;
-    auto offer = [&](float v, int c) {
+    float bar = fmaxf(fmaxf(w.bars[0], w.bars[1]), fmaxf(w.bars[2], w.bars[3]));
+    if (most >= bar) {
+        const int at = atomicAdd(&w.n_lanes, 1);
+        w.lanes[at] = tid;
+        w.maxima[at] = most;
+    }
+    auto offer = [&](float v, int c) {                      // `bar` may rise between calls
         if (!(v >= bar)) return;
         const int at = atomicAdd(&w.n_found, 1);
         if (at < FOUND) w.found[at] = make_float2(v, __int_as_float(c));
@@ -426,9 +429,29 @@ __device__ void part_top(TopScratch &w, const Segment<T, SEGS> &g, float most, i
     __syncthreads();
     const int each = (g.v1 - g.part0 + g.STEP - 1) / g.STEP * AHEAD;       // vectors of a lane, at most
     const int n_lanes = w.n_lanes;
+    // where each has many columns, only the lanes of the k largest maxima (8192
+    // rows of 100003, 20 alternatives: 524 us without this)
+    const bool narrow = each > 16 && n_lanes <= 4 * k;
+    if (narrow) {
+        if (tid < n_lanes) {
+            const float mine = w.maxima[tid];
+            int ahead = 0, level = 0;
+#pragma unroll 8
+            for (int j = 0; j < n_lanes; j++) {
+                ahead += w.maxima[j] > mine;
+                level += w.maxima[j] == mine;
+            }
+            if (ahead < k) w.kept[atomicAdd(&w.n_kept, 1)] = w.lanes[tid];
+            if (ahead < k && ahead + level >= k) w.bars[0] = mine;      // the k-th largest; equal lanes write the same
+        }
+        __syncthreads();
+        bar = w.bars[0];
+    }
+    const int *owners = narrow ? w.kept : w.lanes;
+    const int n_owners = narrow ? w.n_kept : n_lanes;
     if (n_lanes <= 4 * k)
-        for (int i = tid; i < n_lanes * each; i += 256) {
-            const int owner = w.lanes[i / each], n = i % each;
+        for (int i = tid; i < n_owners * each; i += 256) {
+            const int owner = owners[i / each], n = i % each;
             const int v = g.part0 + n / AHEAD * g.STEP + owner / WAVE * g.CHUNK + n % AHEAD * WAVE + owner % WAVE;
             if (v >= g.v1) continue;
             const auto p = g.vector(v);
@@ -492,9 +515,9 @@ __global__ void __launch_bounds__(256) logprob_kernel(LogpArgs a)
     const int row = a.splits > 1 ? (int)blockIdx.x / a.splits : (int)blockIdx.x, split = (int)blockIdx.x - row * a.splits;
     const R *x = (const R *)a.x + row * a.stride;
     const int64_t token = a.tokens[row];
-    const float logit = token >= 0 && token < a.vocab ? (float)x[token] : 0.0f;
     const Segment<T, SEGS> g(x, (int)a.vocab, __builtin_amdgcn_readfirstlane(wave), split, a.splits);
     Stat s = segment_stat<T, SEGS>(g);
+    const float logit = token >= 0 && token < a.vocab ? (float)x[token] : 0.0f;      // here: behind the row's loads
     const float most = s.m;
     s = join_wave(s);
     if (lane == 0) {
@@ -517,22 +540,22 @@ __global__ void __launch_bounds__(256) logprob_kernel(LogpArgs a)
         o[0] = s.m;
         o[1] = s.l;
         o[2] = s.w;
+        o[3] = logit;
     }
     if (TOP && lane < a.top) a.part_top[(int64_t)blockIdx.x * a.top + lane] = best;
 }
 
 // The parts of a row that several workgroups read (at most 64): the
 // alternatives by counting how many of all parts' are ahead of each.
-template <typename T, bool TOP>
+template <bool TOP>
 __global__ void __launch_bounds__(256) logprob_join(LogpArgs a)
 {
-    using R = typename T::raw;
-    __shared__ float2 all[64 * 32];
+    __shared__ uint64_t all[64 * 32];
     __shared__ float2 best[32];
     const int tid = threadIdx.x, lane = tid % WAVE;
     const int64_t row = blockIdx.x;
     const int64_t token = a.tokens[row];
-    const float logit = token >= 0 && token < a.vocab ? (float)((const R *)a.x)[row * a.stride + token] : 0.0f;
+    const float logit = a.part[row * a.splits * 4 + 3];
     Stat s = {LOWEST, 0, 0};
     if (lane < a.splits) {
         const float *o = a.part + (row * a.splits + lane) * 4;
@@ -540,20 +563,20 @@ __global__ void __launch_bounds__(256) logprob_join(LogpArgs a)
     }
     if (TOP) {
         const int n = a.splits * a.top;
-        for (int i = tid; i < n; i += 256) all[i] = a.part_top[row * n + i];
+        // an entry as one number that orders as (value, lower column first) does; none: 0
+        for (int i = tid; i < n; i += 256) {
+            const float2 e = a.part_top[row * n + i];
+            const uint32_t v = __float_as_uint(e.x), up = v & 0x80000000u ? ~v : v | 0x80000000u;
+            all[i] = __float_as_int(e.y) < 0 ? 0 : (uint64_t)up << 32 | ~__float_as_uint(e.y);
+        }
         if (tid < 32) best[tid] = make_float2(0, __int_as_float(-1));
         __syncthreads();
         for (int i = tid; i < n; i += 256) {
-            const float2 mine = all[i];
-            if (__float_as_int(mine.y) < 0) continue;
+            const uint64_t mine = all[i];
             int ahead = 0;
 #pragma unroll 8
-            for (int j = 0; j < n; j++) {
-                const float2 o = all[j];
-                ahead += __float_as_int(o.y) >= 0 &&
-                         (o.x > mine.x || (o.x == mine.x && __float_as_int(o.y) < __float_as_int(mine.y)));
-            }
-            if (ahead < a.top) best[ahead] = mine;
+            for (int j = 0; j < n; j++) ahead += all[j] > mine;
+            if (mine && ahead < a.top) best[ahead] = a.part_top[row * n + i];
         }
         __syncthreads();
     }
@@ -573,7 +596,7 @@ template <typename T, bool TOP> hipError_t logprobs_typed(const LogpArgs &a, hip
     logprob_kernel<T, TOP><<<(unsigned)(a.rows * a.splits), 256, 0, st>>>(a);
     if (a.splits > 1) {
         if (hipError_t e = hipGetLastError()) return e;
-        logprob_join<T, TOP><<<(unsigned)a.rows, 256, 0, st>>>(a);
+        logprob_join<TOP><<<(unsigned)a.rows, 256, 0, st>>>(a);
     }
     return hipGetLastError();
 }
