@@ -21,12 +21,34 @@ struct Fp32 { using raw = float; static constexpr int vec = 4; };
 
 template <typename R, int N> struct alignas(16) Pack { R e[N]; };
 
+// A 16-byte access that, with PAST, asks the caches not to keep the line.
+// The launches ask for it where one call's rows in and out are more than the
+// last-level cache holds, which no reader after it could profit from; written
+// lines left there would be put out during the next kernel instead.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename R, int N, bool PAST> __device__ __forceinline__ Pack<R, N> load_pack(const R *p)
+{
+    if (!PAST) return *(const Pack<R, N> *)p;
+    return __builtin_bit_cast(Pack<R, N>, __builtin_nontemporal_load((const u32x4 *)p));
+}
+
+template <typename R, int N, bool PAST> __device__ __forceinline__ void store_pack(R *p, const Pack<R, N> &v)
+{
+    if (PAST)
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4 *)p);
+    else
+        *(Pack<R, N> *)p = v;
+}
+
+constexpr int64_t LAST_CACHE = (int64_t)256 << 20;       // bytes
+
 // ---- dropout ---------------------------------------------------------------
 // out = residual + keep x / (1 - p).  The mask is a hash of the element's
 // number: nothing but x, residual and out crosses the memory bus.  One 64-bit
 // draw (two 64-bit products) makes the mask of two elements.
 
-template <typename T>
+template <typename T, bool PAST>
 __global__ void __launch_bounds__(256) dropout_vector(DropArgs a)
 {
     using R = typename T::raw;
@@ -42,11 +64,21 @@ __global__ void __launch_bounds__(256) dropout_vector(DropArgs a)
             uint64_t d[4];
 #pragma unroll
             for (int i = 0; i < 4; i++) d[i] = mix64(z0 + GOLDEN * i);
+            constexpr int N = T::vec;
             R xs[8], rs[8], os[8];
             const bool whole = c + 8 <= a.cols;
             if (whole) {
-                __builtin_memcpy(xs, __builtin_assume_aligned(x + c, 16), sizeof(xs));
-                if (res) __builtin_memcpy(rs, __builtin_assume_aligned(res + c, 16), sizeof(rs));
+#pragma unroll
+                for (int i = 0; i < 8; i += N) {
+                    const auto p = load_pack<R, N, PAST>(x + c + i);
+                    __builtin_memcpy(xs + i, &p, sizeof(p));
+                }
+                if (res)
+#pragma unroll
+                    for (int i = 0; i < 8; i += N) {
+                        const auto p = load_pack<R, N, PAST>(res + c + i);
+                        __builtin_memcpy(rs + i, &p, sizeof(p));
+                    }
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
@@ -62,7 +94,12 @@ __global__ void __launch_bounds__(256) dropout_vector(DropArgs a)
                 os[e] = (R)v;
             }
             if (whole) {
-                __builtin_memcpy(__builtin_assume_aligned(out + c, 16), os, sizeof(os));
+#pragma unroll
+                for (int i = 0; i < 8; i += N) {
+                    Pack<R, N> p;
+                    __builtin_memcpy(&p, os + i, sizeof(p));
+                    store_pack<R, N, PAST>(out + c + i, p);
+                }
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; e++)
@@ -95,11 +132,15 @@ __global__ void __launch_bounds__(256) dropout_scalar(DropArgs a)
 
 template <typename T> hipError_t dropout_typed(const DropArgs &a, hipStream_t st)
 {
+    // 32768 rows of 8192 in 16 bits: with the residual 343 -> 314 us, without it 204 -> 193
+    const bool past = a.rows * a.cols * (int64_t)sizeof(typename T::raw) * (a.residual ? 3 : 2) > LAST_CACHE;
     const int64_t items = a.vector ? (a.cols + 7) / 8 : a.cols;
     const unsigned gx = (unsigned)std::min<int64_t>((items + 255) / 256, a.rows > 1 ? 64 : 8192);
     const unsigned gy = (unsigned)std::min<int64_t>(a.rows, 32768);
-    if (a.vector)
-        dropout_vector<T><<<dim3(gx, gy), 256, 0, st>>>(a);
+    if (a.vector && past)
+        dropout_vector<T, true><<<dim3(gx, gy), 256, 0, st>>>(a);
+    else if (a.vector)
+        dropout_vector<T, false><<<dim3(gx, gy), 256, 0, st>>>(a);
     else
         dropout_scalar<T><<<dim3(gx, gy), 256, 0, st>>>(a);
     return hipGetLastError();
@@ -285,7 +326,7 @@ constexpr int AHEAD = 4;
 
 // A wavefront's share of a row's part: chunks of four 16-byte vectors a lane,
 // the workgroup's WAVES wavefronts in turn, so that a workgroup reads one
-// stretch of memory.  Columns before the row's first 16-byte boundary go to
+// stretch of memory.  Columns before the row's first 128-byte boundary go to
 // the first wavefront of the first part, those after its last whole vector to
 // the last of the last.
 template <typename T, int WAVES> struct Segment {
@@ -297,9 +338,10 @@ template <typename T, int WAVES> struct Segment {
 
     __device__ Segment(const R *row, int vocab, int wave, int part, int parts) : x(row)
     {
-        const int mis = (int)((uintptr_t)row % 16 / sizeof(R));
-        head = min(mis ? N - mis : 0, vocab);
-        const int vecs = (vocab - head) / N, per = parts > 1 ? (vecs + parts - 1) / parts : vecs;
+        constexpr int LINE = 128 / sizeof(R);
+        const int mis = (int)((uintptr_t)row % 128 / sizeof(R));
+        head = min(mis ? LINE - mis : 0, vocab);
+        const int vecs = (vocab - head) / N, per = parts > 1 ? (vecs + parts * 8 - 1) / (parts * 8) * 8 : vecs;
         part0 = min(per * part, vecs);
         v0 = part0 + wave * CHUNK;
         v1 = min(part0 + per, vecs);
@@ -310,8 +352,15 @@ template <typename T, int WAVES> struct Segment {
     __device__ Pack<R, N> vector(int v) const { return *(const Pack<R, N> *)(x + head + (int64_t)v * N); }
 };
 
-template <typename T, int WAVES>
-__device__ __forceinline__ Stat segment_stat(const Segment<T, WAVES> &g)
+// What a lane knows of its own columns (edges aside): the largest, the chunk
+// that it is in, and the largest of the other chunks.
+struct LaneTop {
+    float best, second;
+    int chunk;
+};
+
+template <typename T, int WAVES, bool TOP>
+__device__ __forceinline__ Stat segment_stat(const Segment<T, WAVES> &g, LaneTop &top)
 {
     using R = typename T::raw;
     constexpr int N = T::vec;
@@ -323,6 +372,7 @@ __device__ __forceinline__ Stat segment_stat(const Segment<T, WAVES> &g)
         for (int i = 0; i < AHEAD; i++)
             if (v + i * WAVE + lane < g.v1) ahead[i] = g.vector(v + i * WAVE + lane);
     };
+    top = {-INFINITY, -INFINITY, 0};
     load(g.v0);
     for (int v = g.v0; v < g.v1; v += g.STEP) {
         float e[AHEAD][N];
@@ -333,8 +383,14 @@ __device__ __forceinline__ Stat segment_stat(const Segment<T, WAVES> &g)
             for (int j = 0; j < N; j++) e[i][j] = in ? (float)ahead[i].e[j] : -INFINITY;
         }
         load(v + g.STEP);
+        float most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < AHEAD; i++) stat_step(s, e[i]);
+        for (int i = 0; i < AHEAD; i++) most = fmaxf(most, stat_step(s, e[i]));
+        if (TOP) {
+            top.second = fmaxf(top.second, fminf(top.best, most));
+            top.chunk = most > top.best ? v : top.chunk;
+            top.best = fmaxf(top.best, most);
+        }
     }
     if (g.first && lane < g.head) {
         const float e[1] = {(float)g.x[lane]};
@@ -379,18 +435,23 @@ __device__ Top segment_top(const Segment<T, WAVES> &g, int k)
 
 // A workgroup's alternatives among its part of a row.  The statistics' pass
 // has left each lane the maximum of its own columns: a wavefront's k-th
-// largest of these bounds the part's k-th largest element from below, and only
-// the lanes that reach the best of the four bounds (at most 4 k, more where
-// maxima are equal) own elements that do.  Their columns are read again, and
-// of the few elements found each counts how many are ahead of it.  Where more
-// are found than there is room for, as among many equal ones, or fewer than k
-// numbers, the wavefronts' lists do it instead.
+// largest of these bounds the part's k-th largest element from below.  Of the
+// lanes that reach the best of the four bounds (at most 4 k, more where maxima
+// are equal), those of the k largest maxima own all elements that can count.
+// The chunk of a lane's maximum is read again (all of its chunks, if the
+// largest of the others reaches the bar), and of the few elements found each
+// counts how many are ahead of it.  Where more are found than there is room
+// for, as among many equal ones, or fewer than k numbers, the wavefronts'
+// lists do it instead.
 constexpr int FOUND = 512;
 
 struct TopScratch {
     float bars[SEGS];
-    int lanes[256], kept[128];
-    float maxima[256];
+    struct {
+        int lane, chunk;
+        float best, second;
+    } lanes[256];
+    int kept[128];
     float2 found[FOUND];
     float2 lists[SEGS][32];
     float2 best[32];                     // the result: value, column (as bits; -1: none), largest first
@@ -398,10 +459,11 @@ struct TopScratch {
 };
 
 template <typename T>
-__device__ void part_top(TopScratch &w, const Segment<T, SEGS> &g, float most, int k)
+__device__ void part_top(TopScratch &w, const Segment<T, SEGS> &g, const LaneTop &top, int k)
 {
     constexpr int N = T::vec;
     const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE;
+    const float most = top.best;
     // each wavefront's k-th largest lane; the largest of these bounds the row's
     int rank = 0;
 #pragma unroll 8
@@ -416,8 +478,7 @@ __device__ void part_top(TopScratch &w, const Segment<T, SEGS> &g, float most, i
     float bar = fmaxf(fmaxf(w.bars[0], w.bars[1]), fmaxf(w.bars[2], w.bars[3]));
     if (most >= bar) {
         const int at = atomicAdd(&w.n_lanes, 1);
-        w.lanes[at] = tid;
-        w.maxima[at] = most;
+        w.lanes[at] = {tid, top.chunk, most, top.second};
     }
     auto offer = [&](float v, int c) {                      // `bar` may rise between calls
         if (!(v >= bar)) return;
@@ -427,37 +488,37 @@ __device__ void part_top(TopScratch &w, const Segment<T, SEGS> &g, float most, i
     if (g.first && lane < g.head) offer((float)g.x[lane], lane);
     if (lane < g.tails) offer((float)g.x[g.tail0 + lane], g.tail0 + lane);
     __syncthreads();
-    const int each = (g.v1 - g.part0 + g.STEP - 1) / g.STEP * AHEAD;       // vectors of a lane, at most
     const int n_lanes = w.n_lanes;
-    // where each has many columns, only the lanes of the k largest maxima (8192
-    // rows of 100003, 20 alternatives: 524 us without this)
-    const bool narrow = each > 16 && n_lanes <= 4 * k;
-    if (narrow) {
+    if (n_lanes <= 4 * k) {
+        // the lanes of the k largest maxima, and the k-th of those as the bar
         if (tid < n_lanes) {
-            const float mine = w.maxima[tid];
+            const float mine = w.lanes[tid].best;
             int ahead = 0, level = 0;
 #pragma unroll 8
             for (int j = 0; j < n_lanes; j++) {
-                ahead += w.maxima[j] > mine;
-                level += w.maxima[j] == mine;
+                ahead += w.lanes[j].best > mine;
+                level += w.lanes[j].best == mine;
             }
-            if (ahead < k) w.kept[atomicAdd(&w.n_kept, 1)] = w.lanes[tid];
-            if (ahead < k && ahead + level >= k) w.bars[0] = mine;      // the k-th largest; equal lanes write the same
+            if (ahead < k) w.kept[atomicAdd(&w.n_kept, 1)] = tid;
+            if (ahead < k && ahead + level >= k) w.bars[0] = mine;      // equal lanes write the same
         }
         __syncthreads();
         bar = w.bars[0];
-    }
-    const int *owners = narrow ? w.kept : w.lanes;
-    const int n_owners = narrow ? w.n_kept : n_lanes;
-    if (n_lanes <= 4 * k)
-        for (int i = tid; i < n_owners * each; i += 256) {
-            const int owner = owners[i / each], n = i % each;
-            const int v = g.part0 + n / AHEAD * g.STEP + owner / WAVE * g.CHUNK + n % AHEAD * WAVE + owner % WAVE;
-            if (v >= g.v1) continue;
-            const auto p = g.vector(v);
+        // their vectors: of the chunk with the largest, or of all chunks where another one reaches the bar
+        const int chunks = (g.v1 - g.part0 + g.STEP - 1) / g.STEP, n_kept = w.n_kept;
+        for (int i = tid / AHEAD; i < n_kept; i += 256 / AHEAD) {
+            const auto &own = w.lanes[w.kept[i]];
+            const int base = own.lane / WAVE * g.CHUNK + own.lane % WAVE + tid % AHEAD * WAVE;
+            const bool all = own.second >= bar;
+            for (int c = 0; c < (all ? chunks : 1); c++) {
+                const int v = (all ? g.part0 + c * g.STEP : own.chunk - own.lane / WAVE * g.CHUNK) + base;
+                if (v >= g.v1) continue;
+                const auto p = g.vector(v);
 #pragma unroll
-            for (int e = 0; e < N; e++) offer((float)p.e[e], g.head + v * N + e);
+                for (int e = 0; e < N; e++) offer((float)p.e[e], g.head + v * N + e);
+            }
         }
+    }
     __syncthreads();
     const int n = w.n_found;
     if (n_lanes <= 4 * k && n <= FOUND && n >= k) {
@@ -472,15 +533,15 @@ __device__ void part_top(TopScratch &w, const Segment<T, SEGS> &g, float most, i
             if (ahead < k) w.best[ahead] = mine;
         }
     } else {
-        Top top = segment_top<T, SEGS>(g, k);
-        if (lane < k) w.lists[wave][lane] = make_float2(top.value, __int_as_float(top.column));
+        Top list = segment_top<T, SEGS>(g, k);
+        if (lane < k) w.lists[wave][lane] = make_float2(list.value, __int_as_float(list.column));
         __syncthreads();
         if (wave == 0) {
             for (int i = 1; i < SEGS; i++) {
                 const float2 t = lane < k ? w.lists[i][lane] : make_float2(0, __int_as_float(-1));
-                join_list(top, t.x, __float_as_int(t.y), k);
+                join_list(list, t.x, __float_as_int(t.y), k);
             }
-            if (lane < k) w.best[lane] = make_float2(top.value, __int_as_float(top.column));
+            if (lane < k) w.best[lane] = make_float2(list.value, __int_as_float(list.column));
         }
     }
     __syncthreads();
@@ -497,7 +558,8 @@ __global__ void __launch_bounds__(256) logprob_short(LogpArgs a)
     const int64_t token = a.tokens[row];
     const float logit = token >= 0 && token < a.vocab ? (float)x[token] : 0.0f;
     const Segment<T, 1> g(x, (int)a.vocab, 0, 0, 1);
-    const Stat s = join_wave(segment_stat<T, 1>(g));
+    LaneTop unused;
+    const Stat s = join_wave(segment_stat<T, 1, false>(g, unused));
     Top top;
     top.clear();
     if (TOP) top = segment_top<T, 1>(g, a.top);
@@ -516,16 +578,16 @@ __global__ void __launch_bounds__(256) logprob_kernel(LogpArgs a)
     const R *x = (const R *)a.x + row * a.stride;
     const int64_t token = a.tokens[row];
     const Segment<T, SEGS> g(x, (int)a.vocab, __builtin_amdgcn_readfirstlane(wave), split, a.splits);
-    Stat s = segment_stat<T, SEGS>(g);
+    LaneTop lane_top;
+    Stat s = segment_stat<T, SEGS, TOP>(g, lane_top);
     const float logit = token >= 0 && token < a.vocab ? (float)x[token] : 0.0f;      // here: behind the row's loads
-    const float most = s.m;
     s = join_wave(s);
     if (lane == 0) {
         part[wave][0] = s.m;
         part[wave][1] = s.l;
         part[wave][2] = s.w;
     }
-    if (TOP) part_top<T>(scratch, g, most, a.top);
+    if (TOP) part_top<T>(scratch, g, lane_top, a.top);
     else __syncthreads();
     if (wave) return;
     s = {part[0][0], part[0][1], part[0][2]};
@@ -606,7 +668,7 @@ template <typename T, bool TOP> hipError_t logprobs_typed(const LogpArgs &a, hip
 // One read and one write of the row; the few columns that get a term of their
 // own are written once more, after the barrier, by the workgroup that owns them.
 
-template <typename T>
+template <typename T, bool PAST>
 __global__ void __launch_bounds__(256) logprob_grad(LogpGradArgs a, int64_t per)
 {
     using R = typename T::raw;
@@ -638,7 +700,7 @@ __global__ void __launch_bounds__(256) logprob_grad(LogpGradArgs a, int64_t per)
             Pack<R, N> o;
 #pragma unroll
             for (int i = 0; i < N; i++) o.e[i] = (R)value((float)p.e[i]);
-            *(Pack<R, N> *)(dx + c0 + head + v * N) = o;
+            store_pack<R, N, PAST>(dx + c0 + head + v * N, o);
         }
         if (tail0 + threadIdx.x < c1) dx[tail0 + threadIdx.x] = (R)value((float)x[tail0 + threadIdx.x]);
     } else {
@@ -659,10 +721,16 @@ __global__ void __launch_bounds__(256) logprob_grad(LogpGradArgs a, int64_t per)
 
 template <typename T> hipError_t logprobs_grad_typed(const LogpGradArgs &a, hipStream_t st)
 {
+    // 4096 rows of 32000 in 16 bits: this kernel 80 us with and without, the
+    // forward kernel of the next step 76 -> 54 us
+    const bool past = a.rows * a.vocab * (int64_t)sizeof(typename T::raw) * 2 > LAST_CACHE;
     const int64_t per = 8192;                                      // columns of a workgroup
     const unsigned gx = (unsigned)((a.vocab + per - 1) / per);
     const unsigned gy = (unsigned)std::min<int64_t>(a.rows, 32768), gz = (unsigned)((a.rows + gy - 1) / gy);
-    logprob_grad<T><<<dim3(gx, gy, gz), 256, 0, st>>>(a, per);
+    if (past)
+        logprob_grad<T, true><<<dim3(gx, gy, gz), 256, 0, st>>>(a, per);
+    else
+        logprob_grad<T, false><<<dim3(gx, gy, gz), 256, 0, st>>>(a, per);
     return hipGetLastError();
 }
 

@@ -532,6 +532,22 @@ def test_dropout_drops_anything(ops):
     assert ops.dropout_add(torch.empty(0, 5, device="cuda"), p=0.5, seed=1).shape == (0, 5)
 
 
+def test_more_than_the_caches_hold(ops):
+    """Rows in and out of more than 256 MiB: the same bits as a few of the rows by themselves."""
+    torch.manual_seed(3)
+    x = torch.randn(8200, 8203, device="cuda", dtype=torch.bfloat16)
+    for t in (x, x[:, :8200], x[:, 3:8195]):                    # one long row, rows of odd and of even addresses
+        whole, few = (ops.dropout_add(u, u, p=0.1, seed=5) for u in (t, t[:70]))
+        assert torch.equal(whole[:70], few)
+        big, small = t.detach().requires_grad_(), t[:70].detach().requires_grad_()
+        ids = torch.randint(0, t.shape[1], (8200,), device="cuda")
+        a, b = ops.token_logprobs(big, ids), ops.token_logprobs(small, ids[:70])
+        (a.logp.sum() + a.entropy.sum()).backward()
+        (b.logp.sum() + b.entropy.sum()).backward()
+        torch.testing.assert_close(a.logp[:70], b.logp, rtol=2 ** -20, atol=2 ** -20)   # few rows are split further
+        torch.testing.assert_close(big.grad[:70].float(), small.grad.float(), rtol=2 ** -7, atol=2 ** -30)
+
+
 def test_dropout_parts_make_the_whole(ops):
     """Calls whose offsets follow one another draw what one call draws."""
     x = torch.randn(1000, 64, device="cuda", dtype=BF)
