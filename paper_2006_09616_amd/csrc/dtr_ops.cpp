@@ -74,14 +74,18 @@ struct Plan {
 // units, parts for one round of them (12 units of 30011 keys: 33 us with 504
 // workgroups, 39 with 696); beyond, where lengths are many and unequal, for
 // two (256 units of 8192 to 16384 keys: 287 us with 1024, 319 with 512).  A
-// part has 512 keys at least.
-//   Others: parts for two rounds of one workgroup, 256 keys at least.
+// part has 128 keys at least (8 units of 4096 keys: 11 us; 15 with 512 keys,
+// 14 with 64), and 512 keys are one part (7.9 us; 8.5 in four).
+//   Others: parts for two rounds of one workgroup, 256 keys at least (33 rows
+// of 8 units, 4096 keys: 14 us; 17 with 384), and 1024 keys are one part (1024
+// rows of 8 units: 18 us, in four parts 23; 2048 keys in parts: 30 against 31).
 int32_t splits_for(int64_t units, int64_t rows, int64_t k_len)
 {
     const bool few = rows <= FEW_ROWS;
     const int64_t groups = std::max<int64_t>(few ? units : units * ((rows + ROW_TILE - 1) / ROW_TILE), 1);
     const int64_t want = few ? (groups <= 128 ? 512 : 1024) / groups : groups >= 256 ? 1 : (512 + groups - 1) / groups;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(want, k_len / (few ? 512 : 256)), 256));
+    if (k_len <= (few ? 512 : 1024)) return 1;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(want, k_len / (few ? 128 : 256)), 256));
 }
 
 // Parts that the rows are cut into for dK and dV.  A key block's work ranges
@@ -191,10 +195,12 @@ int check_logprobs(int32_t type, int64_t rows, int64_t vocab, int32_t top)
 
 // Parts of a row read by workgroups of their own: one workgroup a row leaves
 // the card idle where there are few rows.  A part has at least 4096 columns,
-// and a row 64 parts at most.
+// and a row 64 parts at most.  64 rows of 131072, 32 bits: 9.8 us, in one part
+// 22; of 32768: 6.8 and 8.0; of 16384: 6.3 and 5.7.  255 rows of 65536: 17 and
+// 14.
 int32_t logprob_splits(int64_t rows, int64_t vocab)
 {
-    if (rows >= 256 || vocab < 8192) return 1;
+    if (rows > 128 || vocab < 24576) return 1;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((512 + rows - 1) / rows, 64), vocab / 4096));
 }
 

@@ -650,8 +650,13 @@ __global__ void __launch_bounds__(256) logprob_join(LogpArgs a)
 
 template <typename T, bool TOP> hipError_t logprobs_typed(const LogpArgs &a, hipStream_t st)
 {
-    // short rows: a wavefront each
-    if (a.vocab <= (int64_t)4 * WAVE * T::vec) {
+    // Short rows: a wavefront each, of up to 8 vectors a lane (4096 rows of 4096
+    // in 16 bits: 10 us, by workgroups 13; of 8192 no gain).  Its alternatives
+    // are a serial list, so that these want shorter rows, the shorter the fewer
+    // there are (8 of 1024: 4096 rows 20 us and 27, 64 rows 13 us and 9; of 512:
+    // 14 and 27, 9.1 and 8.5).
+    const int64_t vectors = !TOP ? 8 : a.rows > 1024 ? 2 : 1;
+    if (a.vocab <= vectors * WAVE * T::vec) {
         logprob_short<T, TOP><<<(unsigned)((a.rows + SEGS - 1) / SEGS), 256, 0, st>>>(a);
         return hipGetLastError();
     }

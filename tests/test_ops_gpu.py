@@ -643,6 +643,16 @@ def test_logprobs_sizes(ops, dtype):
             check_logprobs(ops, x, tok, min(V, 0 if V % 2 else 5), f"{dtype} T {T} V {V}")
 
 
+@pytest.mark.parametrize("dtype", [BF, FP, F32])
+@pytest.mark.parametrize("T,V,top", [(1030, 1000, 20), (1024, 1000, 7), (3, 40002, 5), (128, 24576, 2), (129, 24580, 0)])
+def test_logprobs_rows(ops, dtype, T, V, top):
+    """Numbers of rows about the limits of what works on a row."""
+    g = torch.Generator().manual_seed(T)
+    x = (torch.randn(T, V, generator=g) * 3).to(dtype).cuda()
+    tok = torch.randint(0, V, (T,), generator=g).cuda()
+    check_logprobs(ops, x, tok, top, f"{dtype} T {T} V {V}")
+
+
 @pytest.mark.parametrize("top", [1, 2, 20, 32])
 @pytest.mark.parametrize("order", ["random", "rising", "falling", "equal", "two values"])
 def test_logprobs_alternatives(ops, top, order):
