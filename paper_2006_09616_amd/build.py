@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -18,24 +20,56 @@ OPS_SOURCE = os.path.join(CSRC, "ops_torch.cpp")
 OPS_OUT = os.path.join(HERE, "_ops.so")
 ARCH = "gfx950"
 
-FLAGS = ["-O3", "-std=c++17", "-fPIC", "-shared", f"--offload-arch={ARCH}",
+FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          # no packed FP32 instructions anywhere in the device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-         "-I", os.path.join(ROOT, "include")]
+         # m0 on a clobber list is meant
+         "-Wno-inline-asm",
+         "-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics", "-I", os.path.join(ROOT, "include")]
+
+
+def scratch_of(lines, source: str) -> list:
+    """The kernels of a source that the compiler's remarks give scratch memory, with its bytes a lane."""
+    name, found = "?", []
+    for l in lines:
+        if source not in l or ": remark: " not in l:
+            continue
+        text = l.split(": remark: ")[1].split(" [-R")[0].strip()
+        if text.startswith("Function Name:"):
+            name = text.split(":", 1)[1].strip()
+        if text.startswith("ScratchSize") and text.split(":")[1].strip() != "0":
+            found.append(f"{name}: {text}")
+    return found
 
 
 def build(verbose: bool = False, profile: bool = False) -> str:
     out = OUT_PROFILE if profile else OUT
     tmp = out + ".tmp"
-    cmd = ["hipcc", *FLAGS, *(["-DDTR_PROFILE"] if profile else []), "-o", tmp, *SOURCES]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    noise = [l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l and l.strip()]
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + "\n".join(noise))
-    if verbose and noise:
-        print("\n".join(noise), file=sys.stderr)
+    flags = [*FLAGS, *(["-DDTR_PROFILE"] if profile else [])]
+    with tempfile.TemporaryDirectory() as where:
+        objects = [os.path.join(where, os.path.basename(s) + ".o") for s in SOURCES]
+        commands = [["hipcc", *flags, "-c", "-o", o, s] for o, s in zip(objects, SOURCES)]
+        if verbose:
+            print("\n".join(" ".join(c) for c in commands), flush=True)
+        with ThreadPoolExecutor(len(commands)) as pool:
+            results = list(pool.map(lambda c: subprocess.run(c, capture_output=True, text=True), commands))
+        lines = [l for r in results for l in r.stderr.splitlines()]
+        noise = [l for l in lines if l.strip() and "packed-fp32-ops" not in l and ": remark: " not in l]
+        if any(r.returncode for r in results):
+            raise RuntimeError("hipcc failed:\n" + "\n".join(noise))
+        spilled = scratch_of(lines, "attention.hip")
+        if spilled:
+            # attention's loads into LDS are not the compiler's: a build that put
+            # registers into scratch memory beside them has given wrong gradients
+            raise RuntimeError("attention kernels use scratch memory:\n" + "\n".join(spilled))
+        if verbose and noise:
+            print("\n".join(noise), file=sys.stderr)
+        link = ["hipcc", "-fPIC", "-shared", f"--offload-arch={ARCH}", "-o", tmp, *objects]
+        if verbose:
+            print(" ".join(link), flush=True)
+        res = subprocess.run(link, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stderr)
     os.replace(tmp, out)
     return out
 

@@ -183,7 +183,10 @@ template <int NB> struct Tile {
 // lane; the swizzle is in the addresses that the lanes read.  Reads go through
 // a buffer descriptor of the rows up to `end`: beyond them, and for columns
 // from head_dim on, it delivers zeros.  The compiler does not see these loads:
-// moved() waits for them, before the barrier that hands the tile over.
+// moved() waits for them, before the barrier that hands the tile over.  Nor
+// does it know that what it places before is read by a memory instruction at
+// once: one needs a wait state after a write of m0, and five after a vector
+// instruction has written its scalar operands.
 constexpr int STAGE_ROWS = 64;
 static_assert(STAGE_ROWS == KEY_TILE, "a tile of keys is moved at once");
 
@@ -218,7 +221,7 @@ template <int NB> struct Mover {
         const uint32_t at = lds_address(tile) + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) * 1024;
 #pragma unroll
         for (int n = 0; n < N; n++)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                          :: "s"(at + n * 4096), "v"(offset + n * step), "s"(rsrc) : "memory", "m0");
     }
 };

@@ -148,3 +148,14 @@ def test_logprobs_arguments_refused(lib):
     refused(lib.dtr_logprobs_backward(0, 2, 8, 0, p, 8, p, p, p, None, p, p, None, None, 8, None), "null")
     refused(lib.dtr_logprobs_backward(0, 2, 8, 0, p, 8, p, p, p, None, p, p, None, p, 7, None), "strides")
     assert lib.dtr_logprobs_forward(0, 0, 8, 0, None, 8, None, None, None, None, None, None, None, 0, None) == D.DTR_OK
+
+
+def test_build_finds_scratch_memory():
+    from paper_2006_09616_amd import build as B
+    lines = ["/x/attention.hip:9:1: remark: Function Name: first [-Rpass-analysis=kernel-resource-usage]",
+             "/x/attention.hip:9:1: remark:     ScratchSize [bytes/lane]: 0 [-Rpass-analysis=kernel-resource-usage]",
+             "/x/attention.hip:12:1: remark: Function Name: second [-Rpass-analysis=kernel-resource-usage]",
+             "/x/attention.hip:12:1: remark:     ScratchSize [bytes/lane]: 164 [-Rpass-analysis=kernel-resource-usage]",
+             "/x/replay.hip:5:1: remark:     ScratchSize [bytes/lane]: 48 [-Rpass-analysis=kernel-resource-usage]"]
+    assert B.scratch_of(lines, "attention.hip") == ["second: ScratchSize [bytes/lane]: 164"]
+    assert B.scratch_of(lines[:2], "attention.hip") == []
