@@ -548,6 +548,45 @@ def test_more_than_the_caches_hold(ops):
         torch.testing.assert_close(big.grad[:70].float(), small.grad.float(), rtol=2 ** -7, atol=2 ** -30)
 
 
+def test_offsets_beyond_32_bits(ops):
+    """Rows so far apart that their offsets pass 2^31 elements: the bits of the same rows laid together."""
+    step = 2 ** 23 + 8
+    flat = torch.empty(300 * step, device="cuda", dtype=BF)
+    assert flat.numel() > 2 ** 31
+    torch.manual_seed(4)
+
+    def spread(t, at):                                   # [300, columns] into rows `step` apart
+        view = flat[at:].as_strided(t.shape, (step, 1))
+        view.copy_(t)
+        return view
+
+    k, v = torch.randn(300, 64, device="cuda", dtype=BF), torch.randn(300, 64, device="cuda", dtype=BF)
+    far = [spread(k, 0)[None, :, None], spread(v, 64)[None, :, None]]
+    for Sq in (1, 300):
+        q = torch.randn(1, Sq, 4, 64, device="cuda", dtype=BF)
+        results = []
+        for kk, vv in (far, [k[None, :, None], v[None, :, None]]):
+            ins = [t.detach().requires_grad_() for t in (q, kk, vv)]
+            out = ops.attention(*ins, causal=True)
+            results.append([out, *torch.autograd.grad(out, ins, q)])
+        for a, b in zip(*results):
+            assert torch.equal(a, b), Sq
+    x, ids = torch.randn(300, 1000, device="cuda", dtype=BF), torch.arange(300, device="cuda")
+    results = []
+    for t in (spread(x, 128), x):
+        t = t.detach().requires_grad_()
+        r = ops.token_logprobs(t, ids, top=3)
+        results.append([*r, *torch.autograd.grad((r.logp.sum(), r.top_logp.sum()), t)])
+    for a, b in zip(*results):
+        torch.testing.assert_close(a, b, rtol=2 ** -7 if a.dtype == BF else 2 ** -20, atol=2 ** -20)  # sums in another order
+    del flat, far, results, t, r, a, b, kk, vv, ins, out
+    n = 2 ** 32
+    long = torch.ones(n + 64, device="cuda", dtype=BF)
+    out = ops.dropout_add(long, p=0.5, seed=11)
+    assert torch.equal(out[n - 64:], ops.dropout_add(long[n - 64:], p=0.5, seed=11, offset=(n - 64) // 2))
+    assert torch.equal(out[:64], ops.dropout_add(long[:64], p=0.5, seed=11))
+
+
 def test_dropout_parts_make_the_whole(ops):
     """Calls whose offsets follow one another draw what one call draws."""
     x = torch.randn(1000, 64, device="cuda", dtype=BF)
