@@ -145,8 +145,9 @@ __device__ __forceinline__ float other_half(float x)
     return __uint_as_float(threadIdx.x & 32 ? r[0] : r[1]);
 }
 
-// tanh(x) = 1 - 2 / (1 + exp(2 x)), with x2 = 2 log2(e) x
-__device__ __forceinline__ float tanh_of(float x2) { return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + exp2_(x2)); }
+// (tanh(x) - 1) / 2 = -1 / (1 + exp(2 x)), with x2 = 2 log2(e) x: of this h
+// tanh is 1 + 2 h and its derivative 1 - tanh^2 is -4 (h + h^2)
+__device__ __forceinline__ float minus_half(float x2) { return __builtin_amdgcn_rcpf(-1.0f - exp2_(x2)); }
 
 // A tile in LDS: rows of PITCH 16-bit elements as chunks of 16 bytes, chunk c
 // of row r at c ^ swizzle(r).  Reads of a row's chunk by 16 consecutive rows,
@@ -444,10 +445,13 @@ __device__ __forceinline__ void add_nonfinite(const AttnArgs &a, const char *vb,
 }
 
 // The scores of a lane's keys (key0 + 4 (lane / 32) + 32 (i / 16) + 8 (i % 16 / 4)
-// + i % 4), shaped in place: times log2(e), capped, biased.
+// + i % 4), shaped in place: times log2(e), capped, biased.  apply_but leaves
+// a gain and an offset to the exponent's fma: with a cap alone the scores are
+// then minus_half (8192 tokens in three documents: 303 us, by apply 318; where
+// reading the keys is the bound it only costs registers).
 struct Shape {
     bool capped, bias;
-    float scale2, cap2, slope2;
+    float scale2, cap2, slope2, gain, offset;
     __device__ Shape(const AttnArgs &a, int head)
     {
         capped = a.cap > 0;
@@ -455,12 +459,14 @@ struct Shape {
         slope2 = bias ? a.slopes[head] * LOG2E : 0.0f;
         scale2 = capped ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E;
         cap2 = a.cap * LOG2E;
+        gain = capped && !bias ? 2.0f * cap2 : 1.0f;
+        offset = capped && !bias ? cap2 : 0.0f;
     }
     template <int N> __device__ void apply(float (&x)[N], int distance0) const
     {
         if (capped) {
 #pragma unroll
-            for (int i = 0; i < N; i++) x[i] = cap2 * tanh_of(x[i] * scale2);
+            for (int i = 0; i < N; i++) x[i] = fmaf(minus_half(x[i] * scale2), 2.0f * cap2, cap2);
         } else {
 #pragma unroll
             for (int i = 0; i < N; i++) x[i] *= scale2;
@@ -469,6 +475,15 @@ struct Shape {
             const float pf = (float)distance0;
 #pragma unroll
             for (int i = 0; i < N; i++) x[i] -= slope2 * fabsf(pf - (float)(32 * (i / 16) + 8 * (i % 16 / 4) + i % 4));
+        }
+    }
+    template <int N> __device__ void apply_but(float (&x)[N], int distance0) const
+    {
+        if (capped && !bias) {
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = minus_half(x[i] * scale2);
+        } else {
+            apply(x, distance0);
         }
     }
 };
@@ -483,12 +498,12 @@ struct Shape {
 // its way from memory while one is worked on (two buffers, one barrier a
 // tile).  Rows are packed over the heads of a group, so that shared keys are
 // read once for all of them.
-//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 306 us, 0.90 PFLOP/s of
+//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 316 us, 0.87 PFLOP/s of
 // the visible half; a large product reaches 1.19 to 1.35 on this card.  The
 // rest is the softmax between the two products: the vector unit and the matrix
 // unit of a wavefront take turns, and two wavefronts a unit overlap in part.
 // With a cap the vector unit bounds it: three transcendental instructions a
-// score instead of one (8192 tokens in three documents, 16 heads over 4: 309
+// score instead of one (8192 tokens in three documents, 16 heads over 4: 303
 // us, 0.45 PFLOP/s).
 
 template <typename T, int NB, bool SHAPED>
@@ -573,15 +588,15 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
             interleave<0, 8, 1, 0>();
             // x: the scores times log2(e); plain ones but for a factor left to the exponent's fma
             float x[32];
-            const float gain = SHAPED ? 1.0f : shape.scale2;
+            const float gain = SHAPED ? shape.gain : shape.scale2, offset = SHAPED ? shape.offset : 0.0f;
 #pragma unroll
             for (int i = 0; i < 32; i++) x[i] = s[i / 16][i % 16];
-            if (SHAPED) shape.apply(x, w.pos - j0 - 4 * hi);
+            if (SHAPED) shape.apply_but(x, w.pos - j0 - 4 * hi);
             if (!whole) w.mask(a, x, j0 + 4 * hi, -INFINITY);
             float most = x[0];
 #pragma unroll
             for (int i = 1; i < 32; i++) most = fmaxf(most, x[i]);
-            most = fmaxf(most, other_half(most)) * gain;
+            most = fmaf(fmaxf(most, other_half(most)), gain, offset);
             // The sums are moved to a new maximum only where the old one would let
             // them grow by more than 2^8: 32-bit sums have room, and a probability
             // is rounded relative to itself.
@@ -594,7 +609,7 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
             }
 #pragma unroll
             for (int i = 0; i < 32; i++) {
-                x[i] = exp2_(fmaf(x[i], gain, -m));
+                x[i] = exp2_(fmaf(x[i], gain, offset - m));
                 l += x[i];
             }
 #pragma unroll
@@ -887,8 +902,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
 // product: dQ and dK are then up to 1.5 times as far from the exact gradient as
 // their own rounding makes them (0.0025 against 0.0017 of its norm in bf16).
 // The other way, dS in two parts, costs every such product twice.
-//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 420 us for three products
-// (0.98 PFLOP/s); 8192 tokens in three documents, capped: 385 us.  Bound by the
+//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 430 us for three products
+// (0.96 PFLOP/s); 8192 tokens in three documents, capped: 387 us.  Bound by the
 // matrix unit, whose clock falls under load, and with a cap by the vector unit.
 
 template <typename T, int NB, bool CAP, bool BIAS>
@@ -985,13 +1000,13 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
                     float y;
-                    x[i] = dp[i] - delta;
                     if (CAP) {
-                        const float th = tanh_of(s[i] * scale2);
-                        y = fmaf(cap2, th, -lse2);
-                        x[i] *= fmaf(-th, th, 1.0f);
+                        const float h = minus_half(s[i] * scale2);
+                        y = fmaf(h, 2.0f * cap2, cap2 - lse2);
+                        x[i] = fmaf(dp[i], -4.0f, 4.0f * delta) * fmaf(h, h, h);
                     } else {
                         y = fmaf(s[i], scale2, -lse2);
+                        x[i] = dp[i] - delta;
                     }
                     if (BIAS) y -= slope2 * fabsf(pf - (float)(8 * (i / 4) + i % 4));
                     x[i] *= exp2_(y);
@@ -1026,9 +1041,9 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 // are added up by grad_join_kernel.  Keys and values stay in registers as
 // operands, dK and dV as accumulators: from 65 columns on one workgroup a
 // compute unit.
-//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 690 us for four products
-// (0.80 PFLOP/s); 8192 tokens in three documents, 16 heads over 4, capped: 620
-// us and 32 for the join.  A cap and a bias are template arguments: with both tested in the loop
+//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 740 us for four products
+// (0.74 PFLOP/s; 690 where the clock is not yet down); 8192 tokens in three documents, 16 heads over 4, capped: 627
+// us and 33 for the join.  A cap and a bias are template arguments: with both tested in the loop
 // the accumulators moved between register files at every step.
 template <typename T, int NB, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
@@ -1060,6 +1075,7 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
     }
     const int kdoc = u.docs ? u.docs[min(key, a.k_len - 1)] : 0;
     const float scale2 = CAP ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    constexpr float dp_gain = (CAP ? -4.0f : 1.0f) / T::p_gain;
     f32x16 dk[NB] = {}, dv[NB] = {};
 
     // queries that may see any of the keys: from `first` on, `tiles_q` steps a head
@@ -1133,20 +1149,20 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
     };
     auto store = [&](int buf) {
         if (threadIdx.x < ROWS) {
-            lse2s[buf][threadIdx.x] = stat.x - T::p_shift;
-            deltas[buf][threadIdx.x] = stat.y * (1.0f / T::p_gain);
+            lse2s[buf][threadIdx.x] = stat.x - T::p_shift - (CAP ? cap2 : 0.0f);
+            deltas[buf][threadIdx.x] = stat.y * dp_gain;
             docs[buf][threadIdx.x] = rdoc;
         }
     };
     // probability and score gradient of one element: query qi of the step, of scores s and dP dp
     auto element = [&](float distance, float slope2, float s, float dp, float lse2, float delta, float &p, float &ds)
                        __attribute__((always_inline)) {
-        ds = fmaf(dp, 1.0f / T::p_gain, -delta);
+        ds = fmaf(dp, dp_gain, -delta);
         float y;
         if constexpr (CAP) {
-            const float th = tanh_of(s * scale2);
-            y = fmaf(cap2, th, -lse2);
-            ds *= fmaf(-th, th, 1.0f);
+            const float h = minus_half(s * scale2);
+            y = fmaf(h, 2.0f * cap2, -lse2);
+            ds *= fmaf(h, h, h);
         } else {
             y = fmaf(s, scale2, -lse2);
         }
