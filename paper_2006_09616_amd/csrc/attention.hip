@@ -377,8 +377,8 @@ template <int ROWS, int THREADS> struct RowBlock {
                 atomicMax(&range[1], t);
             }
         __syncthreads();
-        t0 = __builtin_amdgcn_readfirstlane(range[0]);
         t1 = __builtin_amdgcn_readfirstlane(range[1]) + 1;
+        t0 = min(__builtin_amdgcn_readfirstlane(range[0]), t1);      // nothing near: 0, 0
         one_doc = one_doc && doc_lo == doc_hi;
     }
     // whether a tile's documents and the rows' overlap

@@ -840,3 +840,32 @@ def test_refusals(ops):
         with pytest.raises(DtrError) as e:
             bad()
         assert why in str(e.value)
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (FP, 96), (BF, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_few_tokens_with_documents(ops, dtype, D, causal):
+    """Few rows a key head within documents: lengths that end before the queries' document, lengths of zero,
+    positions outside the key slots, keys that no query sees and that are not numbers; whole and split over the keys."""
+    i32 = torch.int32
+    for i, (Sq, Sk, size) in enumerate(((1, 128, 64), (5, 150, 40), (3, 3000, 700), (8, 2050, 64))):
+        B = 5
+        docs = (torch.arange(Sk) // size).to(i32).expand(B, -1).contiguous()   # the same numbers in every request
+        docs[4] = torch.randint(0, 3, (Sk,), generator=torch.Generator().manual_seed(i)).to(i32)
+        short = Sk // size * size - size                  # ends before the last document
+        lengths = torch.tensor([Sk, 0, max(short // 2, 1), short, Sk], dtype=i32)
+        outside = torch.tensor([-40, Sk + 60, -1, Sk - 1, 7], dtype=i32)
+        for name, kw in (("lengths", dict(lengths=lengths)), ("positions outside", dict(starts=outside)),
+                         ("both", dict(lengths=lengths, starts=outside))):
+            q, k, v, do = inputs(B, Sq, Sk, 4, 2, D, dtype, "heads" if i % 2 else "separate", seed=i)
+            start = kw.get("starts", torch.full((B,), Sk - Sq, dtype=i32))
+            for b in range(B):                            # what no query sees may be anything
+                p = torch.arange(Sq) + int(start[b])
+                p = p[(p >= 0) & (p < Sk)]
+                seen = (docs[b][p][:, None] == docs[b][None]) & (not causal or torch.arange(Sk)[None] <= p[:, None])
+                seen &= torch.arange(Sk)[None] < int(kw.get("lengths", torch.full((B,), Sk))[b])
+                hidden = ~seen.any(0).cuda()
+                k.data[b, hidden] = float("nan")
+                v.data[b, hidden] = float("-inf")
+            check(ops, q, k, v, do, f"few tokens, documents, {name} {Sq} {Sk} {D} causal {causal}", causal=causal, docs=docs,
+                  cap=15.0 if i == 1 else 0.0, backward=False, **kw)
