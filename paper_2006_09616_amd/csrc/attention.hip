@@ -1209,12 +1209,19 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
                     p[n] += delta - delta;                 // NaN where it is no number
                 }
             if (!in_doc || jw + 32 > u.end(a, pb)) {
-                // queries of the 32 that see the key: from `from` on
-                const int from = key >= u.len ? INT32_MAX : a.causal && key >= u.prefix ? key - pb - 4 * hi : INT32_MIN;
+                // queries of the 32 that see the key: from `from` on, and before `to`; what
+                // comes after the last query, or with documents has no position in the key
+                // slots, sees nothing
+                int from = key >= u.len ? INT32_MAX : a.causal && key >= u.prefix ? key - pb - 4 * hi : INT32_MIN;
+                int to = a.q_len - st.q0 - 32 * sb - 4 * hi;
+                if (u.docs) {
+                    from = max(from, -pb - 4 * hi);
+                    to = min(to, a.k_len - pb - 4 * hi);
+                }
 #pragma unroll
                 for (int n = 0; n < 16; n++) {
                     const int r = 8 * (n / 4) + n % 4;
-                    const bool seen = (r >= from) & (docs[buf][32 * sb + 4 * hi + r] == kdoc);
+                    const bool seen = (r >= from) & (r < to) & (docs[buf][32 * sb + 4 * hi + r] == kdoc);
                     p[n] = seen ? p[n] : 0.0f;
                     ds[n] = seen ? ds[n] : 0.0f;
                 }

@@ -869,3 +869,49 @@ def test_attention_few_tokens_with_documents(ops, dtype, D, causal):
                 v.data[b, hidden] = float("-inf")
             check(ops, q, k, v, do, f"few tokens, documents, {name} {Sq} {Sk} {D} causal {causal}", causal=causal, docs=docs,
                   cap=15.0 if i == 1 else 0.0, backward=False, **kw)
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (FP, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_gradient_of_queries_outside_the_slots(ops, dtype, D, causal):
+    """With documents a query outside the key slots sees nothing: whatever its gradient is, keys and values get
+    none of it."""
+    Sq, Sk = 150, 130
+    docs = torch.zeros(2, Sk, dtype=torch.int32)
+    docs[1, 60:] = 4
+    starts = torch.tensor([-30, 55], dtype=torch.int32)
+    q, k, v, do = inputs(2, Sq, Sk, 4, 2, D, dtype)
+    pos = torch.arange(Sq)[None] + starts[:, None]
+    outside = ((pos < 0) | (pos >= Sk)).cuda()
+    do = torch.where(outside[:, :, None, None], torch.zeros_like(do), do)
+    want, tol = definition(q, k, v, do, D ** -0.5, 0.0, None, causal, None, docs, None, starts)
+    for bad in (math.nan, math.inf):
+        g = do.clone()
+        g[outside] = bad
+        out = ops.attention(q, k, v, causal=causal, docs=docs.cuda(), starts=starts.cuda())
+        for n, t in zip(("dq", "dk", "dv"), torch.autograd.grad(out, (q, k, v), g)):
+            close(t, want[n], tol[n], f"{n} {bad}")
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (FP, 96), (BF, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_gradients_of_keys_that_nobody_sees(ops, dtype, D, causal):
+    """Keys within the length that no query sees may be anything and get gradients of zero, also where the queries
+    end within a tile."""
+    i32 = torch.int32
+    docs = torch.stack([torch.arange(130) // 40, torch.arange(130) % 3]).to(i32)
+    for name, Sq, kw in (("documents", 5, dict(docs=docs)), ("documents", 70, dict(docs=docs)),
+                         ("starts", 20, dict(starts=torch.tensor([0, 45], dtype=i32))),
+                         ("both", 33, dict(docs=docs, starts=torch.tensor([3, 60], dtype=i32)))):
+        q, k, v, do = inputs(2, Sq, 130, 4, 2, D, dtype)
+        for b in range(2):
+            p = torch.arange(Sq) + int(kw["starts"][b] if "starts" in kw else 130 - Sq)
+            seen = torch.ones(Sq, 130, dtype=torch.bool)
+            if "docs" in kw:
+                seen &= docs[b][p][:, None] == docs[b][None]
+            if causal:
+                seen &= torch.arange(130)[None] <= p[:, None]
+            hidden = ~seen.any(0).cuda()
+            k.data[b, hidden] = float("nan")
+            v.data[b, hidden] = float("inf")
+        check(ops, q, k, v, do, f"nobody sees, {name} {Sq} {D} causal {causal}", causal=causal, **kw)
