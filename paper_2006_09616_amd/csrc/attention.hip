@@ -149,6 +149,29 @@ __device__ __forceinline__ float other_half(float x)
 // tanh is 1 + 2 h and its derivative 1 - tanh^2 is -4 (h + h^2)
 __device__ __forceinline__ float minus_half(float x2) { return __builtin_amdgcn_rcpf(-1.0f - exp2_(x2)); }
 
+// What a cap does with the scores: none, a cap up to LARGE_CAP, a larger one.
+// cap (1 + 2 h) subtracts numbers of the cap's size, so that its error is
+// 1.3e-7 cap whatever the score.  Up to 128 that is below a tenth of fp16's
+// unit (2^-12, as the probabilities are rounded); larger caps take the series
+// of tanh where scores are below a quarter of the cap, and keep the digits of
+// the score.
+enum { PLAIN = 0, SMALL = 1, LARGE = 2 };
+constexpr float LARGE_CAP = 128.0f;
+
+// 1 / cap that leaves a score of zero at zero however small the cap is
+__device__ __forceinline__ float per_cap(float scale, float cap) { return fminf(scale / cap, -LOWEST); }
+
+struct Capped { float score, t; };       // cap tanh(x) in units of log 2, and tanh(x)
+// x tanh's series / x to x^8: 2^-26 at x = 1/4
+__device__ __forceinline__ Capped large_capped(float s, float per_cap, float scale2, float cap2)
+{
+    const float x = s * per_cap, z = x * x;
+    const float f = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 62.0f / 2835, -17.0f / 315), 2.0f / 15), -1.0f / 3), 1.0f);
+    const float h = minus_half(x * (2.0f * LOG2E));
+    const bool near = fabsf(x) < 0.25f;
+    return {near ? s * scale2 * f : fmaf(h, 2.0f * cap2, cap2), near ? x * f : fmaf(h, 2.0f, 1.0f)};
+}
+
 // A tile in LDS: rows of PITCH 16-bit elements as chunks of 16 bytes, chunk c
 // of row r at c ^ swizzle(r).  Reads of a row's chunk by 16 consecutive rows,
 // and of four chunks by four consecutive rows (the transposed reads), then
@@ -448,23 +471,28 @@ __device__ __forceinline__ void add_nonfinite(const AttnArgs &a, const char *vb,
 // + i % 4), shaped in place: times log2(e), capped, biased.  apply_but leaves
 // a gain and an offset to the exponent's fma: with a cap alone the scores are
 // then minus_half (8192 tokens in three documents: 303 us, by apply 318; where
-// reading the keys is the bound it only costs registers).
-struct Shape {
+// reading the keys is the bound it only costs registers).  CAP: LARGE, or else
+// whatever cap there is.
+template <int CAP> struct Shape {
     bool capped, bias;
-    float scale2, cap2, slope2, gain, offset;
+    float scale2, per, cap2, slope2, gain, offset;
     __device__ Shape(const AttnArgs &a, int head)
     {
-        capped = a.cap > 0;
+        capped = CAP != LARGE && a.cap > 0;
         bias = a.slopes != nullptr;
         slope2 = bias ? a.slopes[head] * LOG2E : 0.0f;
-        scale2 = capped ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E;
+        per = per_cap((capped ? 2.0f * LOG2E : 1.0f) * a.scale, a.cap);
+        scale2 = capped ? per : a.scale * LOG2E;
         cap2 = a.cap * LOG2E;
         gain = capped && !bias ? 2.0f * cap2 : 1.0f;
         offset = capped && !bias ? cap2 : 0.0f;
     }
     template <int N> __device__ void apply(float (&x)[N], int distance0) const
     {
-        if (capped) {
+        if (CAP == LARGE) {
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = large_capped(x[i], per, scale2, cap2).score;
+        } else if (capped) {
 #pragma unroll
             for (int i = 0; i < N; i++) x[i] = fmaf(minus_half(x[i] * scale2), 2.0f * cap2, cap2);
         } else {
@@ -506,7 +534,7 @@ struct Shape {
 // score instead of one (8192 tokens in three documents, 16 heads over 4: 303
 // us, 0.45 PFLOP/s).
 
-template <typename T, int NB, bool SHAPED>
+template <typename T, int NB, bool SHAPED, int CAP>
 __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
@@ -538,7 +566,7 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
             q[s] = d < a.head_dim ? *(const s16x8 *)(qp + d * 2) : s16x8{};
         }
     }
-    const Shape shape(a, w.head);
+    const Shape<CAP> shape(a, w.head);
 
     f32x16 o[NB] = {};
     float m = LOWEST, l = 0;
@@ -672,7 +700,7 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
 // 5.5 TB/s of keys and values (a large copy: 4.8).
 constexpr int FEW_WAVES = 4, FEW_KEYS = 32;
 
-template <typename T, int NB, bool SHAPED>
+template <typename T, int NB, bool SHAPED, int CAP>
 __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
@@ -706,7 +734,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
             q[s] = d < a.head_dim ? *(const s16x8 *)(qp + d * 2) : s16x8{};
         }
     }
-    const Shape shape(a, w.head);
+    const Shape<CAP> shape(a, w.head);
     f32x16 o[NB] = {};
     float m = LOWEST, l = 0;
     bool odd = false;                                    // whether cleaned values are to be added
@@ -906,7 +934,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
 // (0.96 PFLOP/s); 8192 tokens in three documents, capped: 387 us.  Bound by the
 // matrix unit, whose clock falls under load, and with a cap by the vector unit.
 
-template <typename T, int NB, bool CAP, bool BIAS>
+template <typename T, int NB, int CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
@@ -946,8 +974,9 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
     const int64_t stat_at = ((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query;
     const float lse = a.lse[stat_at], lse2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
     if (hi == 0 && w.row < a.rows) a.row_stat[stat_at] = make_float2(lse2, delta);
-    const float slope2 = BIAS ? a.slopes[w.head] * LOG2E : 0.0f;
-    const float scale2 = CAP ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    const float slope2 = BIAS && a.slopes ? a.slopes[w.head] * LOG2E : 0.0f;
+    const float scale2 = CAP == SMALL ? per_cap(2.0f * LOG2E * a.scale, a.cap) : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    const float per = per_cap(a.scale, a.cap);
     f32x16 dq[NB] = {};
     const char *kb = head_base(a.k, u.b, u.g), *vb = head_base(a.v, u.b, u.g);
 
@@ -1000,10 +1029,14 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
                     float y;
-                    if (CAP) {
+                    if (CAP == SMALL) {
                         const float h = minus_half(s[i] * scale2);
                         y = fmaf(h, 2.0f * cap2, cap2 - lse2);
                         x[i] = fmaf(dp[i], -4.0f, 4.0f * delta) * fmaf(h, h, h);
+                    } else if (CAP == LARGE) {
+                        const Capped c = large_capped(s[i], per, scale2, cap2);
+                        y = c.score - lse2;
+                        x[i] = (dp[i] - delta) * fmaf(-c.t, c.t, 1.0f);
                     } else {
                         y = fmaf(s[i], scale2, -lse2);
                         x[i] = dp[i] - delta;
@@ -1045,7 +1078,7 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 // (0.74 PFLOP/s; 690 where the clock is not yet down); 8192 tokens in three documents, 16 heads over 4, capped: 627
 // us and 33 for the join.  A cap and a bias are template arguments: with both tested in the loop
 // the accumulators moved between register files at every step.
-template <typename T, int NB, bool CAP, bool BIAS>
+template <typename T, int NB, int CAP, bool BIAS>
 __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
@@ -1074,8 +1107,9 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
         }
     }
     const int kdoc = u.docs ? u.docs[min(key, a.k_len - 1)] : 0;
-    const float scale2 = CAP ? 2.0f * LOG2E * a.scale / a.cap : a.scale * LOG2E, cap2 = a.cap * LOG2E;
-    constexpr float dp_gain = (CAP ? -4.0f : 1.0f) / T::p_gain;
+    const float scale2 = CAP == SMALL ? per_cap(2.0f * LOG2E * a.scale, a.cap) : a.scale * LOG2E, cap2 = a.cap * LOG2E;
+    const float per = per_cap(a.scale, a.cap);
+    constexpr float dp_gain = (CAP == SMALL ? -4.0f : 1.0f) / T::p_gain;
     f32x16 dk[NB] = {}, dv[NB] = {};
 
     // queries that may see any of the keys: from `first` on, `tiles_q` steps a head
@@ -1149,7 +1183,7 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
     };
     auto store = [&](int buf) {
         if (threadIdx.x < ROWS) {
-            lse2s[buf][threadIdx.x] = stat.x - T::p_shift - (CAP ? cap2 : 0.0f);
+            lse2s[buf][threadIdx.x] = stat.x - T::p_shift - (CAP == SMALL ? cap2 : 0.0f);
             deltas[buf][threadIdx.x] = stat.y * dp_gain;
             docs[buf][threadIdx.x] = rdoc;
         }
@@ -1159,10 +1193,14 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
                        __attribute__((always_inline)) {
         ds = fmaf(dp, dp_gain, -delta);
         float y;
-        if constexpr (CAP) {
+        if constexpr (CAP == SMALL) {
             const float h = minus_half(s * scale2);
             y = fmaf(h, 2.0f * cap2, -lse2);
             ds *= fmaf(h, h, h);
+        } else if constexpr (CAP == LARGE) {
+            const Capped c = large_capped(s, per, scale2, cap2);
+            y = c.score - lse2;
+            ds *= fmaf(-c.t, c.t, 1.0f);
         } else {
             y = fmaf(s, scale2, -lse2);
         }
@@ -1180,7 +1218,7 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
             // has what it adds to dK; to dV out . dout takes it (below)
             odd = clean<T, SIZE>(tiles + buf * SIZE, tiles + (2 + buf) * SIZE).b;
         }
-        const float slope2 = BIAS ? a.slopes[u.g * a.group + st.head] * LOG2E : 0.0f;
+        const float slope2 = BIAS && a.slopes ? a.slopes[u.g * a.group + st.head] * LOG2E : 0.0f;
 #pragma unroll 1
         for (int sb = 0; sb < 2; sb++) {
             const int pb = u.start + st.q0 + 32 * sb;
@@ -1246,7 +1284,7 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
     auto whole = [&](const Step &st, int buf) __attribute__((always_inline)) {
         constexpr int M = 4 * NB, AHEAD = 6;              // matrix instructions of a stage
         short *const qt = tiles + buf * SIZE, *const gt = tiles + (2 + buf) * SIZE;
-        const float slope2 = BIAS ? a.slopes[u.g * a.group + st.head] * LOG2E : 0.0f;
+        const float slope2 = BIAS && a.slopes ? a.slopes[u.g * a.group + st.head] * LOG2E : 0.0f;
         const float d0 = (float)(key - u.start - st.q0 - 4 * hi);
         f32x16 s[2] = {}, dp[2] = {};
         f32x4 lse2[2], delta[2];                          // of four queries, and of the next four
@@ -1361,13 +1399,13 @@ hipError_t doc_tiles(const AttnArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-template <typename T, int NB, bool SHAPED> hipError_t forward_sized(const AttnArgs &a, hipStream_t st)
+template <typename T, int NB, bool SHAPED, int CAP> hipError_t forward_sized(const AttnArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
     if (a.rows <= FEW_ROWS)
-        few_rows_kernel<T, NB, SHAPED><<<(unsigned)(units * a.splits), FEW_WAVES * WAVE, 0, st>>>(a);
+        few_rows_kernel<T, NB, SHAPED, CAP><<<(unsigned)(units * a.splits), FEW_WAVES * WAVE, 0, st>>>(a);
     else
-        forward_kernel<T, NB, SHAPED><<<(unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE) * a.splits), 256, 0, st>>>(a);
+        forward_kernel<T, NB, SHAPED, CAP><<<(unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE) * a.splits), 256, 0, st>>>(a);
     if (a.splits > 1) {
         if (hipError_t e = hipGetLastError()) return e;
         join_kernel<T><<<(unsigned)(units * a.rows), 256, 0, st>>>(a);
@@ -1375,7 +1413,7 @@ template <typename T, int NB, bool SHAPED> hipError_t forward_sized(const AttnAr
     return hipGetLastError();
 }
 
-template <typename T, int NB, bool CAP, bool BIAS> hipError_t backward_shaped(const AttnArgs &a, hipStream_t st)
+template <typename T, int NB, int CAP, bool BIAS> hipError_t backward_shaped(const AttnArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
     if (a.rows) {
@@ -1392,16 +1430,20 @@ template <typename T, int NB, bool CAP, bool BIAS> hipError_t backward_shaped(co
 
 template <typename T, int NB> hipError_t backward_sized(const AttnArgs &a, hipStream_t st)
 {
-    if (a.cap > 0) return a.slopes ? backward_shaped<T, NB, true, true>(a, st) : backward_shaped<T, NB, true, false>(a, st);
-    return a.slopes ? backward_shaped<T, NB, false, true>(a, st) : backward_shaped<T, NB, false, false>(a, st);
+    if (a.cap > LARGE_CAP) return backward_shaped<T, NB, LARGE, true>(a, st);        // a bias or none
+    if (a.cap > 0) return a.slopes ? backward_shaped<T, NB, SMALL, true>(a, st) : backward_shaped<T, NB, SMALL, false>(a, st);
+    return a.slopes ? backward_shaped<T, NB, PLAIN, true>(a, st) : backward_shaped<T, NB, PLAIN, false>(a, st);
+}
+
+template <typename T, int NB> hipError_t forward_headed(const AttnArgs &a, hipStream_t st)
+{
+    if (a.cap > LARGE_CAP) return forward_sized<T, NB, true, LARGE>(a, st);
+    return a.cap > 0 || a.slopes ? forward_sized<T, NB, true, SMALL>(a, st) : forward_sized<T, NB, false, PLAIN>(a, st);
 }
 
 template <typename T> hipError_t forward_typed(const AttnArgs &a, hipStream_t st)
 {
-    const bool shaped = a.cap > 0 || a.slopes;
-    if (a.head_dim <= 64) return shaped ? forward_sized<T, 2, true>(a, st) : forward_sized<T, 2, false>(a, st);
-    if (a.head_dim <= 96) return shaped ? forward_sized<T, 3, true>(a, st) : forward_sized<T, 3, false>(a, st);
-    return shaped ? forward_sized<T, 4, true>(a, st) : forward_sized<T, 4, false>(a, st);
+    return a.head_dim <= 64 ? forward_headed<T, 2>(a, st) : a.head_dim <= 96 ? forward_headed<T, 3>(a, st) : forward_headed<T, 4>(a, st);
 }
 
 template <typename T> hipError_t backward_typed(const AttnArgs &a, hipStream_t st)

@@ -915,3 +915,27 @@ def test_attention_gradients_of_keys_that_nobody_sees(ops, dtype, D, causal):
             k.data[b, hidden] = float("nan")
             v.data[b, hidden] = float("inf")
         check(ops, q, k, v, do, f"nobody sees, {name} {Sq} {D} causal {causal}", causal=causal, **kw)
+
+
+@pytest.mark.parametrize("cap", [1e-39, 200.0, 1e3, 1e4, 1e5, 1e7, 1e30, 3e38])
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (FP, 64), (FP, 96), (FP, 128)])
+def test_attention_any_cap(ops, cap, dtype, D):
+    """Scores keep their digits under any cap: the bound is that of scores without one (a large cap hardly changes
+    them, and where scores reach the cap the bound for it is taken).  Terms below the least normal number of 32 bits,
+    2^-126, may count as zero: 150 of at most 4 times that."""
+    least = 2.0 ** -116
+    for i, (Sq, Sk, gain) in enumerate(((150, 150, 1.0), (4, 700, 1.0), (150, 150, 30.0 if cap <= 200 or cap > 1e3 else 8.0))):
+        slopes = torch.tensor([0.5, 0.1, 0.0, 0.01]) if i == 1 or D == 96 else None
+        q, k, v, do = inputs(2, Sq, Sk, 4, 2, D, dtype, seed=i, gain=gain)
+        q.data[0, 1] = 0                                  # scores of exactly zero
+        kw = dict(scale=D ** -0.5, slopes=slopes, causal=True, prefix=None, docs=None, lengths=None, starts=None)
+        rest = [kw[n] for n in ("slopes", "causal", "prefix", "docs", "lengths", "starts")]
+        want, tol = definition(q, k, v, do, D ** -0.5, cap, *rest)
+        if cap >= 1e3:
+            _, tol = definition(q, k, v, do, D ** -0.5, 0.0, *rest)
+        dev = {n: t.cuda() if torch.is_tensor(t) else t for n, t in kw.items()}
+        out, lse = ops.attention(q, k, v, cap=cap, return_lse=True, **dev)
+        close(out, want["out"], tol["out"], f"cap {cap} out {i}")
+        close(lse, want["lse"], tol["lse"], f"cap {cap} lse {i}")
+        for n, t in zip(("dq", "dk", "dv"), torch.autograd.grad(out, (q, k, v), do)):
+            close(t, want[n], tol[n] + least, f"cap {cap} {n} {i}")
