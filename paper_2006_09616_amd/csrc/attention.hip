@@ -33,11 +33,13 @@ struct Bf16 {
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
+    static constexpr bool narrow = false;
     static constexpr float p_gain = 1.0f, p_shift = 0.0f;
     static constexpr uint32_t exponent = 0x7F807F80u, least = 0x00800080u;     // of two numbers, and its lowest bits
 };
 // Backward probabilities of long rows are below the smallest normal number
-// of fp16; 2^6 keeps six more bits of them (they are at most 1).
+// of fp16; 2^6 keeps six more bits of them (they are at most 1).  Score
+// gradients have a range of their own (magnitude_kernel).
 struct Fp16 {
     using raw = _Float16;
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
@@ -45,6 +47,7 @@ struct Fp16 {
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
+    static constexpr bool narrow = true;
     static constexpr float p_gain = 64.0f, p_shift = 6.0f;
     static constexpr uint32_t exponent = 0x7C007C00u, least = 0x04000400u;
 };
@@ -925,6 +928,60 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
 // of all heads of the group.  Seven products instead of five, but every sum
 // has one owner and a fixed order: no atomics, the same bits each time.
 //
+// fp16 holds 2^-24 to 65504: a score gradient dS = P (dP - D) of a long row,
+// or of a small loss, is below that, and one of a scaled loss may be above.
+// |dP| and |D| are at most columns x max |dout| x max |V|, so that a power of
+// two takes the largest possible dS to 2^15: it comes off the 32-bit sums at
+// the end.  Without it dQ over 6000 keys, of a dout of 1e-3, was off by 11 times
+// what its own rounding takes.  A workgroup finds the largest finite number of
+// its chunk of a unit's rows (blockIdx.y 0: values; 1: dout of the group).
+template <typename T>
+__global__ void __launch_bounds__(256) magnitude_kernel(AttnArgs a)
+{
+    __shared__ uint32_t waves[4];
+    const int unit = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+    const Unit u(a, unit);
+    const bool of_v = blockIdx.y == 0;
+    const int64_t n = of_v ? u.len : a.rows, per = (n + a.chunks - 1) / a.chunks, lo = min(per * chunk, n), end = min(lo + per, n);
+    const int pieces = a.head_dim / 8, step = 256 / pieces, piece = threadIdx.x % pieces;
+    uint32_t most = 0;
+    if ((int)threadIdx.x < step * pieces)
+#pragma unroll 4
+        for (int64_t r = lo + threadIdx.x / pieces; r < end; r += step) {
+            const char *p = of_v ? head_base(a.v, u.b, u.g) + r * a.v.position * 2
+                                 : head_base(a.dout, u.b, u.g * a.group + (int)r % a.group) + (int)r / a.group * a.dout.position * 2;
+            const s16x8 v = *(const s16x8 *)(p + piece * 16);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t bits = (uint16_t)v[i] & 0x7FFFu;             // in the order of the numbers
+                most = bits < (T::exponent & 0xFFFFu) ? max(most, bits) : most;
+            }
+        }
+#pragma unroll
+    for (int d = 1; d < WAVE; d *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    if (threadIdx.x % WAVE == 0) waves[threadIdx.x / WAVE] = most;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        a.magnitude[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = max(max(waves[0], waves[1]), max(waves[2], waves[3]));
+}
+
+// the largest of a unit's values (which 0) or gradients (1); a wavefront together
+template <typename T> __device__ __forceinline__ float magnitude(const AttnArgs &a, int unit, int which)
+{
+    const int lane = threadIdx.x % WAVE;
+    const int64_t units = (int64_t)a.batch * a.k_heads;
+    int most = lane < a.chunks ? (int)a.magnitude[(which * units + unit) * a.chunks + lane] : 0;
+#pragma unroll
+    for (int d = 1; d < WAVE; d *= 2) most = max(most, __shfl_xor(most, d));
+    return value_of<T>((short)most);
+}
+// the power of two for score gradients
+__device__ __forceinline__ int gradient_shift(int head_dim, float v, float dout)
+{
+    const float bound = 2.0f * head_dim * v * dout;
+    return bound > 0 && bound < INFINITY ? 15 - __builtin_amdgcn_frexp_expf(bound) : 0;
+}
+
 // Rows of dQ: 128 a workgroup, as the forward pass.  P and dS are 32-bit
 // numbers that are rounded to the inputs' type once, as operands of the last
 // product: dQ and dK are then up to 1.5 times as far from the exact gradient as
@@ -969,11 +1026,21 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
         }
         delta += other_half(delta);
     }
+    int shift = 0;                                       // of the row's score gradients
+    if constexpr (T::narrow) {
+        float most = 0;
+#pragma unroll
+        for (int s = 0; s < 2 * NB; s++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) most = fmaxf(most, fabsf(value_of<T>(g[s][i])));
+        shift = gradient_shift(a.head_dim, magnitude<T>(a, work.unit, 0), fmaxf(most, other_half(most)));
+    }
     // log2-sum-exp2 (plus infinity for a row that sees nothing, so that its P
     // is 0) and D, for the kernel of dK and dV too
     const int64_t stat_at = ((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query;
     const float lse = a.lse[stat_at], lse2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
     if (hi == 0 && w.row < a.rows) a.row_stat[stat_at] = make_float2(lse2, delta);
+    const float shifted = lse2 - (float)shift;
     const float slope2 = BIAS && a.slopes ? a.slopes[w.head] * LOG2E : 0.0f;
     const float scale2 = CAP == SMALL ? per_cap(2.0f * LOG2E * a.scale, a.cap) : a.scale * LOG2E, cap2 = a.cap * LOG2E;
     const float per = per_cap(a.scale, a.cap);
@@ -1031,14 +1098,14 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
                     float y;
                     if (CAP == SMALL) {
                         const float h = minus_half(s[i] * scale2);
-                        y = fmaf(h, 2.0f * cap2, cap2 - lse2);
+                        y = fmaf(h, 2.0f * cap2, cap2 - shifted);
                         x[i] = fmaf(dp[i], -4.0f, 4.0f * delta) * fmaf(h, h, h);
                     } else if (CAP == LARGE) {
                         const Capped c = large_capped(s[i], per, scale2, cap2);
-                        y = c.score - lse2;
+                        y = c.score - shifted;
                         x[i] = (dp[i] - delta) * fmaf(-c.t, c.t, 1.0f);
                     } else {
-                        y = fmaf(s[i], scale2, -lse2);
+                        y = fmaf(s[i], scale2, -shifted);
                         x[i] = dp[i] - delta;
                     }
                     if (BIAS) y -= slope2 * fabsf(pf - (float)(8 * (i / 4) + i % 4));
@@ -1058,13 +1125,14 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
         t = t2;
     }
     if (w.row >= a.rows) return;
+    const float unscale = ldexpf(a.scale, -shift);
 #pragma unroll
     for (int d = 0; d < NB; d++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int col = 32 * d + 8 * e + 4 * hi;
             const f32x4 v = {dq[d][4 * e], dq[d][4 * e + 1], dq[d][4 * e + 2], dq[d][4 * e + 3]};
-            if (col < a.head_dim) write_four<T>(a.dq, u.b, w.head, w.query, col, v * a.scale);
+            if (col < a.head_dim) write_four<T>(a.dq, u.b, w.head, w.query, col, v * unscale);
         }
 }
 
@@ -1109,7 +1177,11 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
     const int kdoc = u.docs ? u.docs[min(key, a.k_len - 1)] : 0;
     const float scale2 = CAP == SMALL ? per_cap(2.0f * LOG2E * a.scale, a.cap) : a.scale * LOG2E, cap2 = a.cap * LOG2E;
     const float per = per_cap(a.scale, a.cap);
-    constexpr float dp_gain = (CAP == SMALL ? -4.0f : 1.0f) / T::p_gain;
+    // of the unit's score gradients; their probability has p_shift already
+    const int shift = T::narrow ? gradient_shift(a.head_dim, magnitude<T>(a, work.unit, 0), magnitude<T>(a, work.unit, 1)) : 0;
+    const float dp_gain = T::narrow ? ldexpf(CAP == SMALL ? -4.0f : 1.0f, __builtin_amdgcn_readfirstlane(shift) - (int)T::p_shift)
+                                    : CAP == SMALL ? -4.0f : 1.0f;
+    const float unscale = T::narrow ? ldexpf(a.scale, -shift) : a.scale;
     f32x16 dk[NB] = {}, dv[NB] = {};
 
     // queries that may see any of the keys: from `first` on, `tiles_q` steps a head
@@ -1365,7 +1437,7 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int col = 32 * d + 8 * e + 4 * hi;
-            f32x4 x = f32x4{dk[d][4 * e], dk[d][4 * e + 1], dk[d][4 * e + 2], dk[d][4 * e + 3]} * a.scale;
+            f32x4 x = f32x4{dk[d][4 * e], dk[d][4 * e + 1], dk[d][4 * e + 2], dk[d][4 * e + 3]} * unscale;
             f32x4 y = f32x4{dv[d][4 * e], dv[d][4 * e + 1], dv[d][4 * e + 2], dv[d][4 * e + 3]} * (1.0f / T::p_gain);
             if (key >= u.len) x = y = f32x4{};            // whatever the queries hold
             if (col >= a.head_dim) continue;
@@ -1416,6 +1488,10 @@ template <typename T, int NB, bool SHAPED, int CAP> hipError_t forward_sized(con
 template <typename T, int NB, int CAP, bool BIAS> hipError_t backward_shaped(const AttnArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
+    if (T::narrow) {
+        magnitude_kernel<T><<<dim3((unsigned)(units * a.chunks), 2), 256, 0, st>>>(a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
     if (a.rows) {
         dq_kernel<T, NB, CAP, BIAS><<<(unsigned)(units * ((a.rows + ROW_TILE - 1) / ROW_TILE)), 256, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;

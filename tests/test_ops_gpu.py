@@ -939,3 +939,51 @@ def test_attention_any_cap(ops, cap, dtype, D):
         close(lse, want["lse"], tol["lse"], f"cap {cap} lse {i}")
         for n, t in zip(("dq", "dk", "dv"), torch.autograd.grad(out, (q, k, v), do)):
             close(t, want[n], tol[n] + least, f"cap {cap} {n} {i}")
+
+
+def whole_sums(q, k, v, do, cap):
+    """Gradients of one head without masks in 64 bits, and the root of the squares of the terms of each."""
+    scale = q.shape[3] ** -0.5
+    q, k, v, do = (t.detach()[0, :, 0].double().cpu() for t in (q, k, v, do))
+    s, dc = scale * q @ k.T, 1.0
+    if cap:
+        t = torch.tanh(s / cap)
+        s, dc = cap * t, 1 - t * t
+    P = torch.softmax(s, 1)
+    dP = do @ v.T
+    dS = P * (dP - (P * dP).sum(1, keepdim=True)) * dc * scale
+    return {"dq": dS @ k, "dk": dS.T @ q, "dv": P.T @ do, "dq noise": ((dS ** 2) @ (k ** 2)).sqrt(),
+            "dk noise": ((dS.T ** 2) @ (q ** 2)).sqrt()}
+
+
+@pytest.mark.parametrize("size", [1e-1, 1e-3, 1e-4, 1e-5])
+@pytest.mark.parametrize("cap", [0.0, 10.0])
+def test_attention_small_gradients_in_fp16(ops, size, cap):
+    """fp16 gradients of a long row lose what rounding them once takes, and what rounding the score gradients by
+    u = 2^-11 each takes (independent errors: their root of squares, at two standard deviations of the largest
+    rounding), however small the output's gradient is."""
+    S, D = 6000, 128
+    q, k, v, do = inputs(1, S, S, 1, 1, D, FP)
+    do.mul_(size / 0.25)
+    want = whole_sums(q, k, v, do, cap)
+    out = ops.attention(q, k, v, cap=cap)
+    grads = dict(zip(("dq", "dk", "dv"), torch.autograd.grad(out, (q, k, v), do)))
+    for n in ("dq", "dk"):
+        exact, noise = want[n], want[n + " noise"]
+        least = (exact.half().double() - exact).norm()
+        err = (grads[n][0, :, 0].double().cpu() - exact).norm()
+        assert err <= 1.1 * least + 2 * U[FP] * noise.norm(), (n, float(err), float(least), float(U[FP] * noise.norm()))
+
+
+def test_attention_large_gradients_in_fp16(ops):
+    """Score gradients beyond fp16's range whose products are within it."""
+    q, k, v, do = inputs(2, 40, 4, 2, 1, 128, FP)
+    v.data.mul_(8)
+    do.mul_(900 / 0.25)
+    out = ops.attention(q, k, v)
+    got = torch.autograd.grad(out, (q, k, v), do)
+    want, tol = definition(q, k, v, do, 128 ** -0.5, 0.0, None, False, None, None, None, None)
+    sizes = {n: want[n].abs().max().item() for n in ("dq", "dk", "dv")}
+    assert max(sizes.values()) < 65000, sizes
+    for n, t in zip(("dq", "dk", "dv"), got):
+        close(t, want[n], tol[n], n)
