@@ -631,10 +631,11 @@ __global__ void __launch_bounds__(256) logprob_join(LogpArgs a)
     }
     if (TOP) {
         const int n = a.splits * a.top;
-        // an entry as one number that orders as (value, lower column first) does; none: 0
+        // an entry as one number that orders as (value, lower column first) does; none: 0.
+        // Minus zero plus zero is zero.
         for (int i = tid; i < n; i += 256) {
             const float2 e = a.part_top[row * n + i];
-            const uint32_t v = __float_as_uint(e.x), up = v & 0x80000000u ? ~v : v | 0x80000000u;
+            const uint32_t v = __float_as_uint(e.x + 0.0f), up = v & 0x80000000u ? ~v : v | 0x80000000u;
             all[i] = __float_as_int(e.y) < 0 ? 0 : (uint64_t)up << 32 | ~__float_as_uint(e.y);
         }
         if (tid < 32) best[tid] = make_float2(0, __int_as_float(-1));

@@ -987,3 +987,17 @@ def test_attention_large_gradients_in_fp16(ops):
     assert max(sizes.values()) < 65000, sizes
     for n, t in zip(("dq", "dk", "dv"), got):
         close(t, want[n], tol[n], n)
+
+
+@pytest.mark.parametrize("T,V", [(2, 300), (3, 5000), (2, 40000), (200, 40000)])
+def test_logprobs_zeros_of_both_signs(ops, T, V):
+    """Minus zero equals zero: the lower column first, in rows read whole and in parts."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.full((T, V), -1.0)
+    at = torch.randint(0, V, (T, 60), generator=g)
+    x.scatter_(1, at, torch.where(torch.rand(T, 60, generator=g) < 0.5, 0.0, -0.0))
+    for dtype in (F32, BF):
+        with torch.no_grad():
+            r = ops.token_logprobs(x.to(dtype).cuda(), torch.zeros(T, dtype=torch.long, device="cuda"), top=12)
+        want = torch.sort(x + 0.0, dim=1, descending=True, stable=True)[1][:, :12]
+        assert torch.equal(r.top_ids.cpu(), want), dtype
