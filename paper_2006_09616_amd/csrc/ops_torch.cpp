@@ -85,15 +85,17 @@ void once(const variable_list &grads)
         if (wants_grad(g)) throw std::runtime_error("the gradients of this operator are not differentiable");
 }
 
-// A tensor of whole numbers for the kernels (int32, contiguous).
-Tensor whole_numbers(const char *name, const OptTensor &o, at::IntArrayRef shape, const Tensor &of)
+// A tensor of whole numbers for the kernels (int32, contiguous): amounts, or
+// names that are only compared.
+Tensor whole_numbers(const char *name, const OptTensor &o, at::IntArrayRef shape, const Tensor &of, bool names = false)
 {
     if (!o || !o->defined()) return Tensor();
     const Tensor &t = *o;
     if (!at::isIntegralType(t.scalar_type(), false)) bad_type(name, " must be a tensor of whole numbers");
     if (t.sizes() != shape) bad_value(name, " has shape ", t.sizes(), ", expected ", shape);
     if (t.device() != of.device()) bad_value(name, " is on ", t.device(), ", the inputs are on ", of.device());
-    if (t.scalar_type() == at::kInt) return t.contiguous();
+    if (names && t.element_size() > 4) bad_type(name, " is ", t.scalar_type(), ", expected numbers of at most 32 bits");
+    if (names || t.scalar_type() == at::kInt) return t.to(at::kInt).contiguous();
     // what int32 cannot hold stays out of range
     return t.to(at::kLong).clamp(std::numeric_limits<int32_t>::min(), std::numeric_limits<int32_t>::max()).to(at::kInt).contiguous();
 }
@@ -232,7 +234,7 @@ std::pair<Tensor, OptTensor> attention(const Tensor &q, const Tensor &k, const T
         o.slopes = slopes->detach().to(at::kFloat).contiguous();
     }
     o.prefix = whole_numbers("prefix", prefix, {B}, q);
-    o.docs = whole_numbers("docs", docs, {B, Sk}, q);
+    o.docs = whole_numbers("docs", docs, {B, Sk}, q, true);
     o.lengths = whole_numbers("lengths", lengths, {B}, q);
     o.starts = whole_numbers("starts", starts, {B}, q);
     if (at::GradMode::is_enabled() && (wants_grad(q) || wants_grad(k) || wants_grad(v))) {

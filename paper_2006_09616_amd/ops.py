@@ -55,7 +55,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, scale: Optio
     slopes   [Hq]: a bias of -slopes[h] * |distance| (a constant: no gradient)
     causal   a query at position p sees keys 0 .. p
     prefix   [B]: keys before prefix[b] are seen by every query (with causal)
-    docs     [B, Sk]: a query sees the keys of its own document only
+    docs     [B, Sk], of at most 32 bits: a query sees the keys of its own
+             document only
     lengths  [B]: keys from lengths[b] on are masked and not read
     starts   [B]: position of the first query, default Sk - Sq (the queries
              are the last key slots).  For new tokens of requests of unequal

@@ -1001,3 +1001,20 @@ def test_logprobs_zeros_of_both_signs(ops, T, V):
             r = ops.token_logprobs(x.to(dtype).cuda(), torch.zeros(T, dtype=torch.long, device="cuda"), top=12)
         want = torch.sort(x + 0.0, dim=1, descending=True, stable=True)[1][:, :12]
         assert torch.equal(r.top_ids.cpu(), want), dtype
+
+
+def test_attention_document_numbers(ops):
+    """Documents are told apart by all bits of their numbers: 8 to 32 bits are taken, 64 refused."""
+    q, k, v, _ = inputs(1, 6, 6, 2, 1, 64, BF)
+    q, k, v = (t.detach() for t in (q, k, v))
+    docs = torch.tensor([[0, 0, 1, 1, 2, 2]], device="cuda")
+    want = ops.attention(q, k, v, docs=docs.to(torch.int32))
+    for t in (torch.int16, torch.int8, torch.uint8):
+        assert torch.equal(ops.attention(q, k, v, docs=docs.to(t)), want)
+    ends = torch.tensor([[-2 ** 31, -2 ** 31, -1, -1, 2 ** 31 - 1, 2 ** 31 - 1]], device="cuda")
+    assert torch.equal(ops.attention(q, k, v, docs=ends.to(torch.int32)), want)
+    for bad in (docs + 2 ** 40, docs):
+        with pytest.raises(TypeError, match="docs"):
+            ops.attention(q, k, v, docs=bad)
+    with pytest.raises(TypeError, match="docs"):
+        ops.attention(q, k, v, docs=docs.float())
