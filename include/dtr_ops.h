@@ -51,6 +51,9 @@ extern "C" {
  * probabilities (and, backward, the gradients of the scores) are rounded to
  * the inputs' type for the matrix instructions.
  * Keys from lengths[b] on are not read (values there may be anything).
+ * Infinities and NaN reach the queries that see them and no others.  Gradients
+ * of a query that has an infinite component, or sees a key with one, may be
+ * NaN where a cap or a probability of zero makes them finite.
  */
 typedef struct {
     int32_t type;               /* DTR_BF16 or DTR_FP16                               */

@@ -990,9 +990,10 @@ __device__ __forceinline__ int gradient_shift(int head_dim, float v, float dout)
 //   4 x 4096 tokens, 16 heads of 128, causal, bf16: 430 us for three products
 // (0.96 PFLOP/s); 8192 tokens in three documents, capped: 387 us.  Bound by the
 // matrix unit, whose clock falls under load, and with a cap by the vector unit.
-
+// Two workgroups a compute unit, but for fp16's large caps at 128 columns: they
+// need 8 bytes a lane more than half of the registers.
 template <typename T, int NB, int CAP, bool BIAS>
-__global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
+__global__ void __launch_bounds__(256, CAP == LARGE && NB == 4 && T::narrow ? 1 : 2) dq_kernel(AttnArgs a)
 {
     using L = Tile<NB>;
     constexpr int SIZE = KEY_TILE * L::PITCH;
@@ -1023,6 +1024,7 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
 #pragma unroll
             for (int i = 0; i < 8; i++)
                 delta += (value_of<T>(o[i]) + value_of<T>(r[i])) * value_of<T>(g[s][i]);
+            if (nonfinite<T>(__builtin_bit_cast(uint4, q[s]))) delta = NAN;
         }
         delta += other_half(delta);
     }
@@ -1064,8 +1066,17 @@ __global__ void __launch_bounds__(256, 2) dq_kernel(AttnArgs a)
         }
         short *const ks = tiles + buf * SIZE, *const vs = tiles + (2 + buf) * SIZE;
         const bool whole = w.whole(t);
-        // a row that sees one of them has it in its log-sum-exp or in out . dout
-        if (w.cut(t)) clean<T, SIZE>(ks, vs);
+        // a row that sees one of them has it in its log-sum-exp or in out . dout, but for
+        // infinite keys whose scores a cap or a probability of zero made finite
+        if (w.cut(t) && clean<T, SIZE>(ks, vs).a) {
+#pragma unroll 1
+            for (int j = j0; j < min(j0 + KEY_TILE, u.len); j++) {
+                bool any = false;
+#pragma unroll 1
+                for (int d = 0; d < a.head_dim; d += 8) any |= nonfinite<T>(*(const uint4 *)(kb + (j * a.k.position + d) * 2));
+                if (any && w.sees(a, j)) delta = NAN;
+            }
+        }
         if (j0 < w.wave_end) {
             // The matrix instructions of both halves of the tile in order: scores
             // and dP, then dQ; operands are read from LDS four ahead (two where
@@ -1288,7 +1299,8 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
         if (!in_doc || min(j0 + GRAD_KEYS, u.len) > u.end(a, u.start + st.q0)) {
             // of a query with one of them, log-sum-exp or out . dout has it, and so
             // has what it adds to dK; to dV out . dout takes it (below)
-            odd = clean<T, SIZE>(tiles + buf * SIZE, tiles + (2 + buf) * SIZE).b;
+            const Odd found = clean<T, SIZE>(tiles + buf * SIZE, tiles + (2 + buf) * SIZE);
+            odd = found.a | found.b;
         }
         const float slope2 = BIAS && a.slopes ? a.slopes[u.g * a.group + st.head] * LOG2E : 0.0f;
 #pragma unroll 1

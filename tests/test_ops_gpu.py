@@ -1018,3 +1018,37 @@ def test_attention_document_numbers(ops):
             ops.attention(q, k, v, docs=bad)
     with pytest.raises(TypeError, match="docs"):
         ops.attention(q, k, v, docs=docs.float())
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (FP, 96), (BF, 128)])
+@pytest.mark.parametrize("what", ["key", "query"])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+def test_attention_gradients_of_infinite_scores(ops, dtype, D, what, cap):
+    """An infinite component of a key or query that a cap, or a probability of zero, makes finite: gradients that
+    come out finite are those of the definition, also where a mask cuts through the tile."""
+    S = 200
+    q, k, v, do = inputs(1, S, S, 2, 1, D, dtype)
+    at = 130                                             # within a tile that the causal mask cuts
+    q.data[..., 3] = q[..., 3].abs() + 0.5
+    k.data[..., 3] = k[..., 3].abs() + 0.5
+    if what == "key":
+        k.data[0, at, 0, 3] = -math.inf
+    else:
+        if not cap:
+            return                                       # its row is not a number throughout
+        q.data[0, at, :, 3] = math.inf
+    want, _ = definition(q, k, v, do, D ** -0.5, cap, None, True, None, None, None, None)
+    big = [t.detach().clone().clamp(-300, 300).requires_grad_() for t in (q, k)]      # scores whose size bounds the errors
+    _, tol = definition(*big, v, do, D ** -0.5, cap, None, True, None, None, None, None)
+    out = ops.attention(q, k, v, cap=cap, causal=True)
+    grads = torch.autograd.grad(out, (q, k, v), do)
+    close(out, want["out"], tol["out"], "out")
+    for n, t in zip(("dq", "dk", "dv"), grads):
+        t = t.double().cpu()
+        both = torch.isfinite(t) & torch.isfinite(want[n])
+        bad = both & ~((t - want[n]).abs() <= tol[n])
+        assert not bad.any(), (n, bad.nonzero()[:4], t[bad][:4], want[n][bad][:4], tol[n][bad][:4])
+        # queries before the key, and keys after the query, do not meet it (above, theirs is 0 x infinity)
+        free, meet = (slice(0, at), slice(at, S)) if n == "dq" else (slice(at + 1, S), slice(0, at + 1))
+        assert not (torch.isfinite(t) & ~torch.isfinite(want[n]))[:, meet].any(), n
+        assert torch.isfinite(t[:, free]).all(), n
