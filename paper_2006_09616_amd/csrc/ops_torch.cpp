@@ -78,11 +78,31 @@ OptTensor maybe(const Tensor &t) { return t.defined() ? OptTensor(t) : std::null
 
 bool wants_grad(const Tensor &t) { return t.defined() && t.requires_grad(); }
 
-void once(const variable_list &grads)
+// Gradients of a backward pass that is recorded (create_graph): they can be
+// used, and refuse to be differentiated rather than count as constants.
+struct Once : torch::autograd::Function<Once> {
+    static Tensor forward(AutogradContext *, const Tensor &made, const OptTensor &, const OptTensor &, const OptTensor &,
+                          const OptTensor &)
+    {
+        return made.detach();
+    }
+    static variable_list backward(AutogradContext *, variable_list)
+    {
+        throw std::runtime_error("the gradients of this operator are not differentiable");
+    }
+};
+
+// `made` out of up to four tensors
+Tensor once(const Tensor &made, const variable_list &from)
 {
-    if (!at::GradMode::is_enabled()) return;
-    for (const Tensor &g : grads)
-        if (wants_grad(g)) throw std::runtime_error("the gradients of this operator are not differentiable");
+    if (!at::GradMode::is_enabled()) return made;
+    bool any = false;
+    OptTensor in[4];
+    for (size_t i = 0; i < from.size(); i++) {
+        any |= wants_grad(from[i]);
+        in[i] = maybe(from[i]);
+    }
+    return any ? Once::apply(made, in[0], in[1], in[2], in[3]) : made;
 }
 
 // A tensor of whole numbers for the kernels (int32, contiguous): amounts, or
@@ -182,7 +202,6 @@ struct Attention : torch::autograd::Function<Attention> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
-        once(grads);
         const variable_list s = ctx->get_saved_variables();
         const AttnOptions o{ctx->saved_data["scale"].toDouble(), ctx->saved_data["cap"].toDouble(),
                             ctx->saved_data["causal"].toBool(), s[6], s[7], s[8], s[9], s[10]};
@@ -199,9 +218,10 @@ struct Attention : torch::autograd::Function<Attention> {
         check(dtr_attn_backward(&a, &hq, &hk, &hv, &ho, ptr(s[5]), (const float *)ptr(s[4]), &hg, &gq, &gk, &gv, ptr(ws),
                                 bytes, stream_of(q)));
         variable_list r(11);
-        r[0] = dq;
-        r[1] = dk;
-        r[2] = dv;
+        const variable_list from = {s[0], s[1], s[2], grads[0]};
+        r[0] = once(dq, from);
+        r[1] = once(dk, from);
+        r[2] = once(dv, from);
         return r;
     }
 };
@@ -300,12 +320,11 @@ struct DropoutAdd : torch::autograd::Function<DropoutAdd> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
-        once(grads);
         variable_list r(5);
         if (!grads[0].defined()) return r;
         if (ctx->needs_input_grad(0))
-            r[0] = dropout(grads[0], Tensor(), ctx->saved_data["p"].toDouble(), (uint64_t)ctx->saved_data["seed"].toInt(),
-                           (uint64_t)ctx->saved_data["offset"].toInt());
+            r[0] = once(dropout(grads[0], Tensor(), ctx->saved_data["p"].toDouble(), (uint64_t)ctx->saved_data["seed"].toInt(),
+                                (uint64_t)ctx->saved_data["offset"].toInt()), {grads[0]});
         if (ctx->saved_data["residual"].toBool() && ctx->needs_input_grad(1)) r[1] = grads[0];
         return r;
     }
@@ -367,7 +386,6 @@ struct TokenLogprobs : torch::autograd::Function<TokenLogprobs> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
-        once(grads);
         const variable_list s = ctx->get_saved_variables();
         const Tensor &x = s[0];
         const int64_t top = ctx->saved_data["top"].toInt();
@@ -380,7 +398,7 @@ struct TokenLogprobs : torch::autograd::Function<TokenLogprobs> {
                                     (const int64_t *)ptr(s[1]), (const float *)ptr(s[2]), (const float *)ptr(s[3]),
                                     (const int64_t *)ptr(s[4]), (const float *)ptr(g[0]), (const float *)ptr(g[1]),
                                     (const float *)ptr(g[2]), ptr(dx), x.size(1), stream_of(x)));
-        return {dx, Tensor(), Tensor()};
+        return {once(dx, {x, grads[0], grads[1], top ? grads[2] : Tensor()}), Tensor(), Tensor()};
     }
 };
 

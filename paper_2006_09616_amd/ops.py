@@ -6,7 +6,8 @@ backward pass can make again.
 ``token_logprobs``   log probabilities of given tokens, entropy, alternatives
 
 All three run on the current stream of their inputs' device, are
-differentiable (once) through ``torch.autograd`` and give the same bits each
+differentiable (once: with create_graph the gradients raise when they are
+differentiated again) through ``torch.autograd`` and give the same bits each
 time they are run on the same inputs, so that a rematerialized call replaces
 the one that was dropped.  The kernels are in ``libdtrsim.so`` behind the C ABI
 of include/dtr_ops.h; ``_ops.so`` puts torch tensors through it.  There is no

@@ -1052,3 +1052,31 @@ def test_attention_gradients_of_infinite_scores(ops, dtype, D, what, cap):
         free, meet = (slice(0, at), slice(at, S)) if n == "dq" else (slice(at + 1, S), slice(0, at + 1))
         assert not (torch.isfinite(t) & ~torch.isfinite(want[n]))[:, meet].any(), n
         assert torch.isfinite(t[:, free]).all(), n
+
+
+def test_gradients_of_gradients_are_refused(ops):
+    """With create_graph the gradients can be used, and refuse to be differentiated again rather than count as
+    constants."""
+    q, k, v, do = inputs(1, 9, 9, 2, 1, 64, BF)
+    x = torch.randn(3, 50, device="cuda", requires_grad=True)
+    tok = torch.tensor([1, 2, 3], device="cuda")
+    plain = torch.autograd.grad(ops.attention(q, k, v), (q, k, v), do)
+    for gdo in (do, do.clone().requires_grad_()):
+        for i, t in enumerate((q, k, v)):
+            g, = torch.autograd.grad(ops.attention(q, k, v), t, gdo, create_graph=True)
+            assert torch.equal(g, plain[i]) and g.requires_grad
+            with pytest.raises(RuntimeError, match="not differentiable"):
+                torch.autograd.grad((g * g).sum() + (q * q).sum() + (k * k).sum() + (v * v).sum(), t)
+    for part in ("logp", "entropy", "top_logp"):
+        g, = torch.autograd.grad(getattr(ops.token_logprobs(x, tok, top=2), part).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="not differentiable"):
+            ((x * x).sum() + (g * g).sum()).backward()
+    # the gradient of dropout does not depend on its input; on the output's gradient it does
+    y = torch.randn(64, device="cuda", requires_grad=True)
+    w = torch.randn(64, device="cuda", requires_grad=True)
+    g, = torch.autograd.grad(ops.dropout_add(y, p=0.5, seed=1), y, torch.ones_like(y), create_graph=True)
+    (y.sum() + g.sum() * 0).backward() if g.requires_grad else y.sum().backward()
+    assert torch.equal(y.grad, torch.ones_like(y))
+    g, = torch.autograd.grad(ops.dropout_add(y, p=0.5, seed=1), y, w, create_graph=True)
+    with pytest.raises(RuntimeError, match="not differentiable"):
+        torch.autograd.grad(g.sum() + w.sum(), w)
