@@ -37,6 +37,12 @@ template <typename... A> std::string text(const A &...a)
 template <typename... A> [[noreturn]] void bad_value(const A &...a) { throw py::value_error(text(a...)); }
 template <typename... A> [[noreturn]] void bad_type(const A &...a) { throw py::type_error(text(a...)); }
 
+[[noreturn]] void unsupported(const char *what)
+{
+    PyErr_SetString(PyExc_NotImplementedError, what);
+    throw py::error_already_set();
+}
+
 void check(int rc)
 {
     if (rc != DTR_OK) throw Failure(rc, dtr_sim_last_error());
@@ -77,6 +83,15 @@ Tensor given(const OptTensor &t) { return t ? *t : Tensor(); }
 OptTensor maybe(const Tensor &t) { return t.defined() ? OptTensor(t) : std::nullopt; }
 
 bool wants_grad(const Tensor &t) { return t.defined() && t.requires_grad(); }
+
+// What would lose the operator's part in silence: a tangent of forward-mode
+// differentiation.
+void no_tangent(std::initializer_list<const Tensor *> inputs)
+{
+    for (const Tensor *t : inputs)
+        if (t->defined() && t->_fw_grad(0).defined())
+            unsupported("the operators have no forward-mode derivatives");
+}
 
 // Gradients of a backward pass that is recorded (create_graph): they can be
 // used, and refuse to be differentiated rather than count as constants.
@@ -244,6 +259,7 @@ std::pair<Tensor, OptTensor> attention(const Tensor &q, const Tensor &k, const T
     const int64_t B = q.size(0), Hq = q.size(2), D = q.size(3), Sk = k.size(1);
     if (k.sizes() != v.sizes() || k.size(0) != B || k.size(3) != D)
         bad_value("shapes ", q.sizes(), ", ", k.sizes(), " and ", v.sizes(), " do not belong together");
+    no_tangent({&q, &k, &v});
     AttnOptions o;
     o.scale = scale ? *scale : D ? 1.0 / std::sqrt((double)D) : 1.0;
     o.cap = cap;
@@ -251,6 +267,7 @@ std::pair<Tensor, OptTensor> attention(const Tensor &q, const Tensor &k, const T
     if (slopes && slopes->defined()) {
         if (slopes->sizes() != at::IntArrayRef({Hq}) || slopes->device() != q.device())
             bad_value("slopes must be [", Hq, "] on ", q.device());
+        no_tangent({&*slopes});
         o.slopes = slopes->detach().to(at::kFloat).contiguous();
     }
     o.prefix = whole_numbers("prefix", prefix, {B}, q);
@@ -338,6 +355,7 @@ Tensor dropout_add(const Tensor &x, const OptTensor &residual, double p, uint64_
     if (r.defined() && (r.sizes() != x.sizes() || r.scalar_type() != x.scalar_type() || r.device() != x.device()))
         bad_value("residual is ", r.sizes(), " ", r.scalar_type(), " on ", r.device(), ", x is ", x.sizes(), " ",
                   x.scalar_type(), " on ", x.device());
+    no_tangent({&x, &r});
     if (!(p >= 0 && p <= 1)) bad_value("probability ", p, " is not within 0..1");
     if (at::GradMode::is_enabled() && (wants_grad(x) || wants_grad(r)))
         return DropoutAdd::apply(x, maybe(r), p, (int64_t)seed, (int64_t)offset);
@@ -413,6 +431,7 @@ py::tuple token_logprobs(const Tensor &logits, const Tensor &tokens, int64_t top
     const int64_t V = logits.size(-1);
     if (V == 0) bad_value("the vocabulary is empty");
     if (top < 0 || top > DTR_TOP_MAX || top > V) bad_value(top, " alternatives of a vocabulary of ", V, " (at most ", DTR_TOP_MAX, ")");
+    no_tangent({&logits});
     Tensor x = logits.dim() == 2 ? logits : logits.reshape({-1, V});
     if (x.stride(1) != 1 && V > 1) x = x.contiguous();
     const Tensor tok = tokens.reshape({-1}).to(at::kLong).contiguous();

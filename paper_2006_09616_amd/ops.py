@@ -13,8 +13,9 @@ the one that was dropped.  The kernels are in ``libdtrsim.so`` behind the C ABI
 of include/dtr_ops.h; ``_ops.so`` puts torch tensors through it.  There is no
 fallback: on anything but a GPU the calls raise.
 
-Errors: ValueError and TypeError for tensors that do not fit together, and
-``dtr.DtrError`` for what the C ABI refuses.
+Errors: ValueError and TypeError for tensors that do not fit together,
+``dtr.DtrError`` for what the C ABI refuses, and NotImplementedError for
+forward-mode differentiation.
 """
 from __future__ import annotations
 

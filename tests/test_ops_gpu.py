@@ -1080,3 +1080,22 @@ def test_gradients_of_gradients_are_refused(ops):
     g, = torch.autograd.grad(ops.dropout_add(y, p=0.5, seed=1), y, w, create_graph=True)
     with pytest.raises(RuntimeError, match="not differentiable"):
         torch.autograd.grad(g.sum() + w.sum(), w)
+
+
+def test_tangents_are_refused(ops):
+    """Forward-mode differentiation is not supported: it raises rather than lose the tangent."""
+    import torch.autograd.forward_ad as fw
+    q, k, v, _ = (t.detach() for t in inputs(1, 9, 9, 2, 1, 64, BF))
+    x = torch.randn(3, 50, device="cuda")
+    tok = torch.tensor([1, 2, 3], device="cuda")
+    slopes = torch.rand(2, device="cuda")
+    with fw.dual_level():
+        def dual(t):
+            return fw.make_dual(t, torch.ones_like(t))
+
+        for call in (lambda: ops.attention(dual(q), k, v), lambda: ops.attention(q, dual(k), v), lambda: ops.attention(q, k, dual(v)),
+                     lambda: ops.attention(q, k, v, slopes=dual(slopes)), lambda: ops.dropout_add(dual(x), p=0.1, seed=1),
+                     lambda: ops.dropout_add(x, dual(x), p=0.1, seed=1), lambda: ops.token_logprobs(dual(x), tok)):
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                call()
+        assert torch.equal(ops.dropout_add(x, p=0.1, seed=1), ops.dropout_add(x.clone(), p=0.1, seed=1))
