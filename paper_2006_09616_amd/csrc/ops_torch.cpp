@@ -4,6 +4,7 @@
 // backward pass in Python alone some 70 us), so this one is C++; every step of
 // the computation is a call of the C ABI.
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
@@ -85,9 +86,11 @@ OptTensor maybe(const Tensor &t) { return t.defined() ? OptTensor(t) : std::null
 bool wants_grad(const Tensor &t) { return t.defined() && t.requires_grad(); }
 
 // What would lose the operator's part in silence: a tangent of forward-mode
-// differentiation.
-void no_tangent(std::initializer_list<const Tensor *> inputs)
+// differentiation, and torch.jit.trace, which records the outputs' allocation
+// and not the kernels that fill them.
+void run_as_it_is(std::initializer_list<const Tensor *> inputs)
 {
+    if (torch::jit::tracer::isTracing()) unsupported("torch.jit.trace does not record the operators");
     for (const Tensor *t : inputs)
         if (t->defined() && t->_fw_grad(0).defined())
             unsupported("the operators have no forward-mode derivatives");
@@ -259,7 +262,7 @@ std::pair<Tensor, OptTensor> attention(const Tensor &q, const Tensor &k, const T
     const int64_t B = q.size(0), Hq = q.size(2), D = q.size(3), Sk = k.size(1);
     if (k.sizes() != v.sizes() || k.size(0) != B || k.size(3) != D)
         bad_value("shapes ", q.sizes(), ", ", k.sizes(), " and ", v.sizes(), " do not belong together");
-    no_tangent({&q, &k, &v});
+    run_as_it_is({&q, &k, &v});
     AttnOptions o;
     o.scale = scale ? *scale : D ? 1.0 / std::sqrt((double)D) : 1.0;
     o.cap = cap;
@@ -267,7 +270,7 @@ std::pair<Tensor, OptTensor> attention(const Tensor &q, const Tensor &k, const T
     if (slopes && slopes->defined()) {
         if (slopes->sizes() != at::IntArrayRef({Hq}) || slopes->device() != q.device())
             bad_value("slopes must be [", Hq, "] on ", q.device());
-        no_tangent({&*slopes});
+        run_as_it_is({&*slopes});
         o.slopes = slopes->detach().to(at::kFloat).contiguous();
     }
     o.prefix = whole_numbers("prefix", prefix, {B}, q);
@@ -355,7 +358,7 @@ Tensor dropout_add(const Tensor &x, const OptTensor &residual, double p, uint64_
     if (r.defined() && (r.sizes() != x.sizes() || r.scalar_type() != x.scalar_type() || r.device() != x.device()))
         bad_value("residual is ", r.sizes(), " ", r.scalar_type(), " on ", r.device(), ", x is ", x.sizes(), " ",
                   x.scalar_type(), " on ", x.device());
-    no_tangent({&x, &r});
+    run_as_it_is({&x, &r});
     if (!(p >= 0 && p <= 1)) bad_value("probability ", p, " is not within 0..1");
     if (at::GradMode::is_enabled() && (wants_grad(x) || wants_grad(r)))
         return DropoutAdd::apply(x, maybe(r), p, (int64_t)seed, (int64_t)offset);
@@ -431,7 +434,7 @@ py::tuple token_logprobs(const Tensor &logits, const Tensor &tokens, int64_t top
     const int64_t V = logits.size(-1);
     if (V == 0) bad_value("the vocabulary is empty");
     if (top < 0 || top > DTR_TOP_MAX || top > V) bad_value(top, " alternatives of a vocabulary of ", V, " (at most ", DTR_TOP_MAX, ")");
-    no_tangent({&logits});
+    run_as_it_is({&logits});
     Tensor x = logits.dim() == 2 ? logits : logits.reshape({-1, V});
     if (x.stride(1) != 1 && V > 1) x = x.contiguous();
     const Tensor tok = tokens.reshape({-1}).to(at::kLong).contiguous();

@@ -15,7 +15,7 @@ fallback: on anything but a GPU the calls raise.
 
 Errors: ValueError and TypeError for tensors that do not fit together,
 ``dtr.DtrError`` for what the C ABI refuses, and NotImplementedError for
-forward-mode differentiation.
+forward-mode differentiation and ``torch.jit.trace``.
 """
 from __future__ import annotations
 

@@ -1099,3 +1099,14 @@ def test_tangents_are_refused(ops):
             with pytest.raises(NotImplementedError, match="forward-mode"):
                 call()
         assert torch.equal(ops.dropout_add(x, p=0.1, seed=1), ops.dropout_add(x.clone(), p=0.1, seed=1))
+
+
+def test_recorded_calls_are_refused(ops):
+    """torch.jit.trace would record the outputs' allocation without the kernels that fill them."""
+    q = torch.randn(1, 5, 2, 64, device="cuda", dtype=BF)
+    x = torch.randn(3, 50, device="cuda")
+    tok = torch.tensor([1, 2, 3], device="cuda")
+    for call, arg in ((lambda t: ops.attention(t, t, t), q), (lambda t: ops.dropout_add(t, p=0.1, seed=1), x),
+                      (lambda t: ops.token_logprobs(t, tok).logp, x)):
+        with pytest.raises(NotImplementedError, match="trace"):
+            torch.jit.trace(call, arg, check_trace=False)
