@@ -375,10 +375,10 @@ LogpResult logprobs_forward(const Tensor &x, const Tensor &tokens, int64_t top)
     const int64_t T = x.size(0), V = x.size(1);
     const auto f32 = x.options().dtype(at::kFloat);
     LogpResult r;
-    const Tensor three = at::empty({3, T}, f32);
-    r.logp = three[0];
-    r.entropy = three[1];
-    r.lse = three[2];
+    // of their own: views of one tensor could not be changed in place
+    r.logp = at::empty({T}, f32);
+    r.entropy = at::empty({T}, f32);
+    r.lse = at::empty({T}, f32);
     if (top) {
         r.top_logp = at::empty({T, top}, f32);
         r.top_ids = at::empty({T, top}, f32.dtype(at::kLong));

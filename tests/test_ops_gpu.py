@@ -1110,3 +1110,25 @@ def test_recorded_calls_are_refused(ops):
                       (lambda t: ops.token_logprobs(t, tok).logp, x)):
         with pytest.raises(NotImplementedError, match="trace"):
             torch.jit.trace(call, arg, check_trace=False)
+
+
+def test_logprobs_scaled_in_place(ops):
+    """Outputs are tensors of their own: log probabilities may be changed in place before the backward pass."""
+    tok = torch.tensor([1, -1, 3, 4], device="cuda")
+    w = torch.tensor([1.0, 0.0, 2.0, -1.0], device="cuda")
+    for T, V in ((4, 60), (4, 50000)):
+        x = torch.randn(T, V, device="cuda", requires_grad=True)
+        r = ops.token_logprobs(x, tok, top=3)
+        want, = torch.autograd.grad((r.logp * w).sum() + r.entropy.sum() + (2 * r.top_logp).sum(), x)
+        r = ops.token_logprobs(x, tok, top=3)
+        r.logp.mul_(w)
+        r.top_logp.mul_(2)
+        got, = torch.autograd.grad(r.logp.sum() + r.entropy.sum() + r.top_logp.sum(), x)
+        assert torch.equal(got, want)
+        r = ops.token_logprobs(x, tok)
+        with torch.no_grad():
+            r.logp.detach().mul_(w)                       # nothing that the backward pass needs
+        torch.autograd.grad(r.logp.sum() + r.entropy.sum(), x)
+        r = ops.token_logprobs(x, tok)
+        for t in (r.logp, r.entropy):
+            assert t._base is None and t.untyped_storage().nbytes() == 4 * T
