@@ -3,6 +3,7 @@
 // more than these kernels do at the sizes of one request or one layer (a
 // backward pass in Python alone some 70 us), so this one is C++; every step of
 // the computation is a call of the C ABI.
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/pybind.h>
@@ -84,6 +85,30 @@ Tensor given(const OptTensor &t) { return t ? *t : Tensor(); }
 OptTensor maybe(const Tensor &t) { return t.defined() ? OptTensor(t) : std::nullopt; }
 
 bool wants_grad(const Tensor &t) { return t.defined() && t.requires_grad(); }
+
+// sets Python's error; under its lock
+void set_error(const Failure &e)
+{
+    const std::string full = e.what(), head = text("dtr_sim error ", e.code, ": ");
+    py::object cls = py::module_::import("paper_2006_09616_amd.dtr").attr("DtrError");
+    py::object err = cls(e.code, full.substr(head.size()));
+    PyErr_SetObject(cls.ptr(), err.ptr());
+}
+
+// A backward pass, whose exceptions reach Python by way of the autograd engine:
+// only Python's own keep their type on it.
+template <typename F> variable_list backward_pass(F f)
+{
+    try {
+        return f();
+    } catch (const Failure &e) {
+        py::gil_scoped_acquire lock;
+        set_error(e);
+        python_error error;
+        error.persist();
+        throw error;
+    }
+}
 
 // What would lose the operator's part in silence: a tangent of forward-mode
 // differentiation, and torch.jit.trace, which records the outputs' allocation
@@ -220,6 +245,11 @@ struct Attention : torch::autograd::Function<Attention> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
+        return backward_pass([&] { return gradients(ctx, grads); });
+    }
+
+    static variable_list gradients(AutogradContext *ctx, const variable_list &grads)
+    {
         const variable_list s = ctx->get_saved_variables();
         const AttnOptions o{ctx->saved_data["scale"].toDouble(), ctx->saved_data["cap"].toDouble(),
                             ctx->saved_data["causal"].toBool(), s[6], s[7], s[8], s[9], s[10]};
@@ -340,6 +370,11 @@ struct DropoutAdd : torch::autograd::Function<DropoutAdd> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
+        return backward_pass([&] { return gradients(ctx, grads); });
+    }
+
+    static variable_list gradients(AutogradContext *ctx, const variable_list &grads)
+    {
         variable_list r(5);
         if (!grads[0].defined()) return r;
         if (ctx->needs_input_grad(0))
@@ -407,6 +442,11 @@ struct TokenLogprobs : torch::autograd::Function<TokenLogprobs> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
+        return backward_pass([&] { return gradients(ctx, grads); });
+    }
+
+    static variable_list gradients(AutogradContext *ctx, const variable_list &grads)
+    {
         const variable_list s = ctx->get_saved_variables();
         const Tensor &x = s[0];
         const int64_t top = ctx->saved_data["top"].toInt();
@@ -472,10 +512,7 @@ PYBIND11_MODULE(_ops, m)
         try {
             if (p) std::rethrow_exception(p);
         } catch (const Failure &e) {
-            const std::string full = e.what(), head = text("dtr_sim error ", e.code, ": ");
-            py::object cls = py::module_::import("paper_2006_09616_amd.dtr").attr("DtrError");
-            py::object err = cls(e.code, full.substr(head.size()));
-            PyErr_SetObject(cls.ptr(), err.ptr());
+            set_error(e);
         }
     });
     m.def("attention", &attention);

@@ -1132,3 +1132,17 @@ def test_logprobs_scaled_in_place(ops):
         r = ops.token_logprobs(x, tok)
         for t in (r.logp, r.entropy):
             assert t._base is None and t.untyped_storage().nbytes() == 4 * T
+
+
+def test_refusals_of_a_backward_pass(ops):
+    """What the C ABI refuses raises DtrError from a backward pass too: here the gradient of keys that lie by heads,
+    whose contiguous positions are too far apart."""
+    from paper_2006_09616_amd.dtr import DtrError
+    H = 2 ** 18
+    q = torch.zeros(1, 1, H, 64, device="cuda", dtype=BF, requires_grad=True)
+    k = torch.zeros(1, H, 2, 64, device="cuda", dtype=BF).transpose(1, 2)
+    out = ops.attention(q, k, k)
+    for _ in range(2):
+        with pytest.raises(DtrError, match="positions of dk") as e:
+            torch.autograd.grad(out, q, torch.ones_like(out), retain_graph=True)
+        assert e.value.code < 0
