@@ -20,6 +20,7 @@ forward-mode differentiation and ``torch.jit.trace``.
 from __future__ import annotations
 
 import os
+from operator import index
 from typing import NamedTuple, Optional
 
 import torch
@@ -83,7 +84,7 @@ def dropout_add(x: torch.Tensor, residual: Optional[torch.Tensor] = None, *, p: 
     offset .. offset + (n + 1) // 2 - 1: calls that share a seed take offsets
     that far apart.  seed and offset count modulo 2^64."""
     m = 0xFFFFFFFFFFFFFFFF
-    return (_binding or lib()).dropout_add(x, residual, p, seed & m, offset & m)
+    return (_binding or lib()).dropout_add(x, residual, p, index(seed) & m, index(offset) & m)
 
 
 class TokenLogprobs(NamedTuple):

@@ -1146,3 +1146,13 @@ def test_refusals_of_a_backward_pass(ops):
         with pytest.raises(DtrError, match="positions of dk") as e:
             torch.autograd.grad(out, q, torch.ones_like(out), retain_graph=True)
         assert e.value.code < 0
+
+
+def test_dropout_seeds_of_any_integer_type(ops):
+    x = torch.randn(100, device="cuda")
+    want = ops.dropout_add(x, p=0.5, seed=12345, offset=7)
+    assert torch.equal(ops.dropout_add(x, p=0.5, seed=np.int64(12345), offset=np.int32(7)), want)
+    assert torch.equal(ops.dropout_add(x, p=0.5, seed=np.int64(-1)), ops.dropout_add(x, p=0.5, seed=2 ** 64 - 1))
+    for bad in (1.5, "7", None):
+        with pytest.raises(TypeError):
+            ops.dropout_add(x, p=0.5, seed=bad)
