@@ -39,7 +39,7 @@ struct Bf16 {
 };
 // Backward probabilities of long rows are below the smallest normal number
 // of fp16; 2^6 keeps six more bits of them (they are at most 1).  Score
-// gradients have a range of their own (magnitude_kernel).
+// gradients have a range of their own (value_magnitude_kernel).
 struct Fp16 {
     using raw = _Float16;
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
@@ -933,24 +933,23 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
 // |dP| and |D| are at most columns x max |dout| x max |V|, so that a power of
 // two takes the largest possible dS to 2^15: it comes off the 32-bit sums at
 // the end.  Without it dQ over 6000 keys, of a dout of 1e-3, was off by 11 times
-// what its own rounding takes.  A workgroup finds the largest finite number of
-// its chunk of a unit's rows (blockIdx.y 0: values; 1: dout of the group).
+// what its own rounding takes.  Here a workgroup finds the largest finite
+// number of its chunk of a unit's values; the gradients of rows that see
+// something are looked at by the kernel of dQ, for that of dK and dV too.
 template <typename T>
-__global__ void __launch_bounds__(256) magnitude_kernel(AttnArgs a)
+__global__ void __launch_bounds__(256) value_magnitude_kernel(AttnArgs a)
 {
     __shared__ uint32_t waves[4];
     const int unit = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
     const Unit u(a, unit);
-    const bool of_v = blockIdx.y == 0;
-    const int64_t n = of_v ? u.len : a.rows, per = (n + a.chunks - 1) / a.chunks, lo = min(per * chunk, n), end = min(lo + per, n);
+    const int per = (u.len + a.chunks - 1) / a.chunks, lo = min(per * chunk, u.len), end = min(lo + per, u.len);
     const int pieces = a.head_dim / 8, step = 256 / pieces, piece = threadIdx.x % pieces;
+    const char *const vb = head_base(a.v, u.b, u.g) + piece * 16;
     uint32_t most = 0;
     if ((int)threadIdx.x < step * pieces)
 #pragma unroll 4
-        for (int64_t r = lo + threadIdx.x / pieces; r < end; r += step) {
-            const char *p = of_v ? head_base(a.v, u.b, u.g) + r * a.v.position * 2
-                                 : head_base(a.dout, u.b, u.g * a.group + (int)r % a.group) + (int)r / a.group * a.dout.position * 2;
-            const s16x8 v = *(const s16x8 *)(p + piece * 16);
+        for (int j = lo + (int)threadIdx.x / pieces; j < end; j += step) {
+            const s16x8 v = *(const s16x8 *)(vb + j * a.v.position * 2);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const uint32_t bits = (uint16_t)v[i] & 0x7FFFu;             // in the order of the numbers
@@ -962,18 +961,26 @@ __global__ void __launch_bounds__(256) magnitude_kernel(AttnArgs a)
     if (threadIdx.x % WAVE == 0) waves[threadIdx.x / WAVE] = most;
     __syncthreads();
     if (threadIdx.x == 0)
-        a.magnitude[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = max(max(waves[0], waves[1]), max(waves[2], waves[3]));
+        a.value_magnitude[blockIdx.x] = value_of<T>((short)max(max(waves[0], waves[1]), max(waves[2], waves[3])));
 }
 
-// the largest of a unit's values (which 0) or gradients (1); a wavefront together
-template <typename T> __device__ __forceinline__ float magnitude(const AttnArgs &a, int unit, int which)
+// the largest of n numbers of at least 0; a wavefront together
+__device__ __forceinline__ float largest(const float *p, int n)
 {
-    const int lane = threadIdx.x % WAVE;
-    const int64_t units = (int64_t)a.batch * a.k_heads;
-    int most = lane < a.chunks ? (int)a.magnitude[(which * units + unit) * a.chunks + lane] : 0;
+    float most = 0;
+    for (int i = threadIdx.x % WAVE; i < n; i += WAVE) most = fmaxf(most, p[i]);
 #pragma unroll
-    for (int d = 1; d < WAVE; d *= 2) most = max(most, __shfl_xor(most, d));
-    return value_of<T>((short)most);
+    for (int d = 1; d < WAVE; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    return most;
+}
+__device__ __forceinline__ float value_magnitude(const AttnArgs &a, int unit)
+{
+    return largest(a.value_magnitude + (int64_t)unit * a.chunks, a.chunks);
+}
+// of the gradients of a row tile, a number a wavefront
+__device__ __forceinline__ float *row_magnitude(const AttnArgs &a, int unit, int tile)
+{
+    return a.row_magnitude + ((int64_t)unit * ((a.rows + ROW_TILE - 1) / ROW_TILE) + tile) * 4;
 }
 // the power of two for score gradients
 __device__ __forceinline__ int gradient_shift(int head_dim, float v, float dout)
@@ -1028,6 +1035,11 @@ __global__ void __launch_bounds__(256, CAP == LARGE && NB == 4 && T::narrow ? 1 
         }
         delta += other_half(delta);
     }
+    // log2-sum-exp2 (plus infinity for a row that sees nothing, so that its P
+    // is 0) and D, for the kernel of dK and dV too
+    const int64_t stat_at = ((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query;
+    const float lse = a.lse[stat_at], lse2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
+    if (hi == 0 && w.row < a.rows) a.row_stat[stat_at] = make_float2(lse2, delta);
     int shift = 0;                                       // of the row's score gradients
     if constexpr (T::narrow) {
         float most = 0;
@@ -1035,13 +1047,13 @@ __global__ void __launch_bounds__(256, CAP == LARGE && NB == 4 && T::narrow ? 1 
         for (int s = 0; s < 2 * NB; s++)
 #pragma unroll
             for (int i = 0; i < 8; i++) most = fmaxf(most, fabsf(value_of<T>(g[s][i])));
-        shift = gradient_shift(a.head_dim, magnitude<T>(a, work.unit, 0), fmaxf(most, other_half(most)));
+        most = fmaxf(most, other_half(most));
+        shift = gradient_shift(a.head_dim, value_magnitude(a, work.unit), most);
+        most = lse2 == INFINITY || most == INFINITY ? 0.0f : most;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        if (lane == 0) row_magnitude(a, work.unit, tile_row / ROW_TILE)[threadIdx.x / WAVE] = most;
     }
-    // log2-sum-exp2 (plus infinity for a row that sees nothing, so that its P
-    // is 0) and D, for the kernel of dK and dV too
-    const int64_t stat_at = ((int64_t)u.b * a.k_heads * a.group + w.head) * a.q_len + w.query;
-    const float lse = a.lse[stat_at], lse2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
-    if (hi == 0 && w.row < a.rows) a.row_stat[stat_at] = make_float2(lse2, delta);
     const float shifted = lse2 - (float)shift;
     const float slope2 = BIAS && a.slopes ? a.slopes[w.head] * LOG2E : 0.0f;
     const float scale2 = CAP == SMALL ? per_cap(2.0f * LOG2E * a.scale, a.cap) : a.scale * LOG2E, cap2 = a.cap * LOG2E;
@@ -1189,7 +1201,8 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
     const float scale2 = CAP == SMALL ? per_cap(2.0f * LOG2E * a.scale, a.cap) : a.scale * LOG2E, cap2 = a.cap * LOG2E;
     const float per = per_cap(a.scale, a.cap);
     // of the unit's score gradients; their probability has p_shift already
-    const int shift = T::narrow ? gradient_shift(a.head_dim, magnitude<T>(a, work.unit, 0), magnitude<T>(a, work.unit, 1)) : 0;
+    const int shift = T::narrow ? gradient_shift(a.head_dim, value_magnitude(a, work.unit),
+                                                 largest(row_magnitude(a, work.unit, 0), (a.rows + ROW_TILE - 1) / ROW_TILE * 4)) : 0;
     const float dp_gain = T::narrow ? ldexpf(CAP == SMALL ? -4.0f : 1.0f, __builtin_amdgcn_readfirstlane(shift) - (int)T::p_shift)
                                     : CAP == SMALL ? -4.0f : 1.0f;
     const float unscale = T::narrow ? ldexpf(a.scale, -shift) : a.scale;
@@ -1501,7 +1514,7 @@ template <typename T, int NB, int CAP, bool BIAS> hipError_t backward_shaped(con
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
     if (T::narrow) {
-        magnitude_kernel<T><<<dim3((unsigned)(units * a.chunks), 2), 256, 0, st>>>(a);
+        value_magnitude_kernel<T><<<(unsigned)(units * a.chunks), 256, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (a.rows) {

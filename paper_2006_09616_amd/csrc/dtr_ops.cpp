@@ -64,7 +64,7 @@ int check_heads(const char *name, const dtr_heads *t, const dtr_attn *a, bool ou
 
 struct Plan {
     int32_t splits, parts, chunks;
-    size_t docs, part_out, part_stat, part_grad, row_stat, magnitude, total;
+    size_t docs, part_out, part_stat, part_grad, row_stat, value_magnitude, row_magnitude, total;
 };
 
 // Parts that the keys are split into.  One part per row tile leaves most of
@@ -122,9 +122,12 @@ Plan make_plan(const dtr_attn *a, bool backward)
     if (backward) {
         p.parts = parts_for(units * ((a->k_len + GRAD_KEYS - 1) / GRAD_KEYS), rows);
         p.row_stat = take(sizeof(float2) * units * rows);
-        // two workgroups a compute unit to read all of v and dout
-        p.chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(units, 1), 64));
-        if (a->type == DTR_FP16) p.magnitude = take(sizeof(uint32_t) * 2 * units * p.chunks);
+        if (a->type == DTR_FP16) {
+            // two workgroups a compute unit to read all of v
+            p.chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(units, 1), 64));
+            p.value_magnitude = take(sizeof(float) * units * p.chunks);
+            p.row_magnitude = take(sizeof(float) * units * ((rows + ROW_TILE - 1) / ROW_TILE) * 4);
+        }
         if (p.parts > 1) p.part_grad = take(sizeof(float) * 2 * p.parts * units * a->k_len * a->head_dim);
     }
     p.total = at;
@@ -160,7 +163,8 @@ AttnArgs make_args(const dtr_attn *a, const Plan &p, char *ws)
     k.part_stat = (float2 *)(ws + p.part_stat);
     k.row_stat = (float2 *)(ws + p.row_stat);
     k.chunks = p.chunks;
-    k.magnitude = (uint32_t *)(ws + p.magnitude);
+    k.value_magnitude = (float *)(ws + p.value_magnitude);
+    k.row_magnitude = (float *)(ws + p.row_magnitude);
     return k;
 }
 

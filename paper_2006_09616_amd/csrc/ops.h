@@ -37,8 +37,9 @@ struct AttnArgs {
     int32_t parts;                // parts that the rows are cut into (dK and dV)
     float *part_grad;             // [parts][2][batch][k_heads][k_len][head_dim] (parts > 1)
     float2 *row_stat;             // [batch][q_heads][q_len] log2-sum-exp2 and out . dout (backward)
-    int32_t chunks;               // at most 64: of a key head's rows, whose largest numbers are looked for (backward, fp16)
-    uint32_t *magnitude;          // [2][batch][k_heads][chunks] largest finite number of v, and of dout, as bits
+    int32_t chunks;               // of a key head's values, whose largest numbers are looked for (backward, fp16)
+    float *value_magnitude;       // [batch][k_heads][chunks] largest finite number of v
+    float *row_magnitude;         // [batch][k_heads][row tiles][4] of dout, 32 rows each
 };
 
 struct LogpArgs {

@@ -1156,3 +1156,23 @@ def test_dropout_seeds_of_any_integer_type(ops):
     for bad in (1.5, "7", None):
         with pytest.raises(TypeError):
             ops.dropout_add(x, p=0.5, seed=bad)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_gradients_beside_rows_that_see_nothing(ops, causal):
+    """Large gradients of queries that see nothing leave the bits of the others' as they are."""
+    Sq, Sk = 150, 130
+    docs = torch.zeros(2, Sk, dtype=torch.int32, device="cuda")
+    docs[1, 60:] = 4
+    starts = torch.tensor([-30, 55], dtype=torch.int32, device="cuda")
+    pos = torch.arange(Sq, device="cuda")[None] + starts[:, None]
+    outside = (pos < 0) | (pos >= Sk)
+    q, k, v, do = inputs(2, Sq, Sk, 4, 2, 64, FP)
+    do.mul_(2.0 ** -12)
+    results = []
+    for other in (0.0, 60000.0):
+        do[outside] = other
+        out = ops.attention(q, k, v, causal=causal, docs=docs, starts=starts)
+        results.append(torch.autograd.grad(out, (q, k, v), do))
+    for n, a, b in zip(("dq", "dk", "dv"), *results):
+        assert torch.equal(a, b), n
