@@ -178,7 +178,7 @@ Tensor rows_of(const Tensor &t)
     bool ok = t.stride(3) == 1 && (uintptr_t)t.data_ptr() % 16 == 0;
     for (int d = 0; d < 3; d++) ok = ok && (t.size(d) == 1 || t.stride(d) % 8 == 0);
     ok = ok && (t.size(1) == 1 || t.stride(1) < (int64_t(1) << 24));
-    return ok ? t : t.contiguous();
+    return ok ? t : t.clone(at::MemoryFormat::Contiguous);     // contiguous() would give a contiguous one back
 }
 
 dtr_heads heads_of(const Tensor &t)

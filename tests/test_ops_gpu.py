@@ -1176,3 +1176,22 @@ def test_attention_gradients_beside_rows_that_see_nothing(ops, causal):
         results.append(torch.autograd.grad(out, (q, k, v), do))
     for n, a, b in zip(("dq", "dk", "dv"), *results):
         assert torch.equal(a, b), n
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 1, 120), (2, 37, 2, 64)])
+def test_attention_contiguous_rows_at_odd_addresses(ops, shape):
+    """Tensors that are contiguous but do not start at a multiple of 16 bytes are copied, too."""
+    def odd(t):
+        flat = torch.empty(t.numel() + 1, device="cuda", dtype=t.dtype)
+        flat[1:] = t.detach().reshape(-1)
+        return flat[1:].view(t.shape)
+
+    B, S, H, D = shape
+    q, k, v, do = inputs(B, S, S, H, H, D, BF)
+    want = ops.attention(q, k, v, causal=True)
+    want = [want, *torch.autograd.grad(want, (q, k, v), do)]
+    ins = [odd(t).requires_grad_() for t in (q, k, v)]
+    assert ins[0].is_contiguous() and ins[0].data_ptr() % 16
+    out = ops.attention(*ins, causal=True)
+    for a, b in zip((out, *torch.autograd.grad(out, ins, odd(do))), want):
+        assert torch.equal(a, b)
