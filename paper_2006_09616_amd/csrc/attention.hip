@@ -1513,7 +1513,7 @@ template <typename T, int NB, bool SHAPED, int CAP> hipError_t forward_sized(con
 template <typename T, int NB, int CAP, bool BIAS> hipError_t backward_shaped(const AttnArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
-    if (T::narrow) {
+    if constexpr (T::narrow) {
         value_magnitude_kernel<T><<<(unsigned)(units * a.chunks), 256, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
     }
