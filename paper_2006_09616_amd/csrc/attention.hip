@@ -474,17 +474,17 @@ __device__ __forceinline__ void add_nonfinite(const AttnArgs &a, const char *vb,
 // + i % 4), shaped in place: times log2(e), capped, biased.  apply_but leaves
 // a gain and an offset to the exponent's fma: with a cap alone the scores are
 // then minus_half (8192 tokens in three documents: 303 us, by apply 318; where
-// reading the keys is the bound it only costs registers).  CAP: LARGE, or else
-// whatever cap there is.
+// reading the keys is the bound it only costs registers).  CAP SMALL stands for
+// a cap, a bias or both.
 template <int CAP> struct Shape {
     bool capped, bias;
     float scale2, per, cap2, slope2, gain, offset;
     __device__ Shape(const AttnArgs &a, int head)
     {
-        capped = CAP != LARGE && a.cap > 0;
+        capped = CAP == SMALL && a.cap > 0;
         bias = a.slopes != nullptr;
         slope2 = bias ? a.slopes[head] * LOG2E : 0.0f;
-        per = per_cap((capped ? 2.0f * LOG2E : 1.0f) * a.scale, a.cap);
+        per = CAP == PLAIN ? 0.0f : per_cap((capped ? 2.0f * LOG2E : 1.0f) * a.scale, a.cap);
         scale2 = capped ? per : a.scale * LOG2E;
         cap2 = a.cap * LOG2E;
         gain = capped && !bias ? 2.0f * cap2 : 1.0f;
