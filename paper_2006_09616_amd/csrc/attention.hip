@@ -937,7 +937,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
 // number of its chunk of a unit's values; the gradients of rows that see
 // something are looked at by the kernel of dQ, for that of dK and dV too.
 template <typename T>
-__global__ void __launch_bounds__(256) value_magnitude_kernel(AttnArgs a)
+__global__ void __launch_bounds__(256) value_magnitude_kernel(AttnGradArgs a)
 {
     __shared__ uint32_t waves[4];
     const int unit = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
@@ -973,12 +973,12 @@ __device__ __forceinline__ float largest(const float *p, int n)
     for (int d = 1; d < WAVE; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
     return most;
 }
-__device__ __forceinline__ float value_magnitude(const AttnArgs &a, int unit)
+__device__ __forceinline__ float value_magnitude(const AttnGradArgs &a, int unit)
 {
     return largest(a.value_magnitude + (int64_t)unit * a.chunks, a.chunks);
 }
 // of the gradients of a row tile, a number a wavefront
-__device__ __forceinline__ float *row_magnitude(const AttnArgs &a, int unit, int tile)
+__device__ __forceinline__ float *row_magnitude(const AttnGradArgs &a, int unit, int tile)
 {
     return a.row_magnitude + ((int64_t)unit * ((a.rows + ROW_TILE - 1) / ROW_TILE) + tile) * 4;
 }
@@ -1000,7 +1000,7 @@ __device__ __forceinline__ int gradient_shift(int head_dim, float v, float dout)
 // Two workgroups a compute unit, but for fp16's large caps at 128 columns: they
 // need 8 bytes a lane more than half of the registers.
 template <typename T, int NB, int CAP, bool BIAS>
-__global__ void __launch_bounds__(256, CAP == LARGE && NB == 4 && T::narrow ? 1 : 2) dq_kernel(AttnArgs a)
+__global__ void __launch_bounds__(256, CAP == LARGE && NB == 4 && T::narrow ? 1 : 2) dq_kernel(AttnGradArgs a)
 {
     using L = Tile<NB>;
     constexpr int SIZE = KEY_TILE * L::PITCH;
@@ -1170,7 +1170,7 @@ __global__ void __launch_bounds__(256, CAP == LARGE && NB == 4 && T::narrow ? 1 
 // us and 33 for the join.  A cap and a bias are template arguments: with both tested in the loop
 // the accumulators moved between register files at every step.
 template <typename T, int NB, int CAP, bool BIAS>
-__global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
+__global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnGradArgs a)
 {
     using L = Tile<NB>;
     constexpr int ROWS = STAGE_ROWS, SIZE = ROWS * L::PITCH;
@@ -1478,7 +1478,7 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnArgs a)
 
 // Adds up the parts of dK (blockIdx.y 0) and dV (1): 8 keys a workgroup, four columns a lane.
 template <typename T>
-__global__ void __launch_bounds__(256) grad_join_kernel(AttnArgs a)
+__global__ void __launch_bounds__(256) grad_join_kernel(AttnGradArgs a)
 {
     const int64_t n = (int64_t)a.batch * a.k_heads * a.k_len, r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
     const int c = threadIdx.x % 32 * 4;
@@ -1510,7 +1510,7 @@ template <typename T, int NB, bool SHAPED, int CAP> hipError_t forward_sized(con
     return hipGetLastError();
 }
 
-template <typename T, int NB, int CAP, bool BIAS> hipError_t backward_shaped(const AttnArgs &a, hipStream_t st)
+template <typename T, int NB, int CAP, bool BIAS> hipError_t backward_shaped(const AttnGradArgs &a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.batch * a.k_heads;
     if constexpr (T::narrow) {
@@ -1529,7 +1529,7 @@ template <typename T, int NB, int CAP, bool BIAS> hipError_t backward_shaped(con
     return hipGetLastError();
 }
 
-template <typename T, int NB> hipError_t backward_sized(const AttnArgs &a, hipStream_t st)
+template <typename T, int NB> hipError_t backward_sized(const AttnGradArgs &a, hipStream_t st)
 {
     if (a.cap > LARGE_CAP) return backward_shaped<T, NB, LARGE, true>(a, st);        // a bias or none
     if (a.cap > 0) return a.slopes ? backward_shaped<T, NB, SMALL, true>(a, st) : backward_shaped<T, NB, SMALL, false>(a, st);
@@ -1547,7 +1547,7 @@ template <typename T> hipError_t forward_typed(const AttnArgs &a, hipStream_t st
     return a.head_dim <= 64 ? forward_headed<T, 2>(a, st) : a.head_dim <= 96 ? forward_headed<T, 3>(a, st) : forward_headed<T, 4>(a, st);
 }
 
-template <typename T> hipError_t backward_typed(const AttnArgs &a, hipStream_t st)
+template <typename T> hipError_t backward_typed(const AttnGradArgs &a, hipStream_t st)
 {
     return a.head_dim <= 64 ? backward_sized<T, 2>(a, st) : a.head_dim <= 96 ? backward_sized<T, 3>(a, st) : backward_sized<T, 4>(a, st);
 }
@@ -1560,7 +1560,7 @@ hipError_t launch_attn_forward(const AttnArgs &a, int type, hipStream_t st)
     return type == 0 ? forward_typed<Bf16>(a, st) : forward_typed<Fp16>(a, st);
 }
 
-hipError_t launch_attn_backward(const AttnArgs &a, int type, hipStream_t st)
+hipError_t launch_attn_backward(const AttnGradArgs &a, int type, hipStream_t st)
 {
     if (hipError_t e = doc_tiles(a, st)) return e;
     return type == 0 ? backward_typed<Bf16>(a, st) : backward_typed<Fp16>(a, st);

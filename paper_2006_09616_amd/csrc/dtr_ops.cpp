@@ -136,9 +136,10 @@ Plan make_plan(const dtr_attn *a, bool backward)
 
 Heads of(const dtr_heads *t) { return t ? Heads{(char *)t->data, t->batch, t->position, t->head} : Heads{}; }
 
-AttnArgs make_args(const dtr_attn *a, const Plan &p, char *ws)
+// what both passes need, and the backward pass besides
+AttnGradArgs make_args(const dtr_attn *a, const Plan &p, char *ws)
 {
-    AttnArgs k{};
+    AttnGradArgs k{};
     k.batch = a->batch;
     k.q_len = a->q_len;
     k.k_len = a->k_len;
@@ -265,7 +266,7 @@ int dtr_attn_backward(const dtr_attn *attn, const dtr_heads *q, const dtr_heads 
     if (int rc = check_workspace(workspace, workspace_bytes, p.total)) return rc;
     if (attn->batch == 0 || (attn->q_len == 0 && attn->k_len == 0)) return DTR_OK;
     if (!lse && attn->q_len) return fail(DTR_EINVAL, "attention: null lse");
-    AttnArgs a = make_args(attn, p, (char *)workspace);
+    AttnGradArgs a = make_args(attn, p, (char *)workspace);
     a.q = of(q);
     a.k = of(k);
     a.v = of(v);

@@ -25,7 +25,7 @@ struct AttnArgs {
     float scale, cap;
     const float *slopes;
     const int32_t *prefix, *docs, *lengths, *starts;
-    Heads q, k, v, out, dout, dq, dk, dv;
+    Heads q, k, v, out;
     char *rest;                   // [batch][q_len][q_heads][head_dim] what rounding took from out, or NULL
     float *lse;                   // [batch][q_heads][q_len]
     int32_t rows;                 // q_len * group: rows of one key head, row = query * group + head of the group
@@ -34,10 +34,16 @@ struct AttnArgs {
     int2 *doc_tiles;              // [batch][key_tiles] smallest and largest document of each tile
     float *part_out;              // [splits][batch][k_heads][rows][head_dim] (splits > 1)
     float2 *part_stat;            // [splits][batch][k_heads][rows] maximum and sum
+};
+
+// What the backward pass needs besides; apart, as the smallest forward calls
+// notice the size of their arguments.
+struct AttnGradArgs : AttnArgs {
+    Heads dout, dq, dk, dv;
     int32_t parts;                // parts that the rows are cut into (dK and dV)
     float *part_grad;             // [parts][2][batch][k_heads][k_len][head_dim] (parts > 1)
-    float2 *row_stat;             // [batch][q_heads][q_len] log2-sum-exp2 and out . dout (backward)
-    int32_t chunks;               // of a key head's values, whose largest numbers are looked for (backward, fp16)
+    float2 *row_stat;             // [batch][q_heads][q_len] log2-sum-exp2 and out . dout
+    int32_t chunks;               // of a key head's values, whose largest numbers are looked for (fp16)
     float *value_magnitude;       // [batch][k_heads][chunks] largest finite number of v
     float *row_magnitude;         // [batch][k_heads][row tiles][4] of dout, 32 rows each
 };
@@ -72,7 +78,7 @@ struct DropArgs {
 };
 
 hipError_t launch_attn_forward(const AttnArgs &a, int type, hipStream_t st);
-hipError_t launch_attn_backward(const AttnArgs &a, int type, hipStream_t st);
+hipError_t launch_attn_backward(const AttnGradArgs &a, int type, hipStream_t st);
 hipError_t launch_logprobs(const LogpArgs &a, int type, hipStream_t st);
 hipError_t launch_logprobs_grad(const LogpGradArgs &a, int type, hipStream_t st);
 hipError_t launch_dropout(const DropArgs &a, int type, hipStream_t st);
