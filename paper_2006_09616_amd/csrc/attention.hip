@@ -34,12 +34,14 @@ struct Bf16 {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
     static constexpr bool narrow = false;
-    static constexpr float p_gain = 1.0f, p_shift = 0.0f;
+    static constexpr float p_gain = 1.0f, p_shift = 0.0f, lift = 0.0f, slack = 8.0f;
     static constexpr uint32_t exponent = 0x7F807F80u, least = 0x00800080u;     // of two numbers, and its lowest bits
 };
-// Backward probabilities of long rows are below the smallest normal number
-// of fp16; 2^6 keeps six more bits of them (they are at most 1).  Score
-// gradients have a range of their own (value_magnitude_kernel).
+// Probabilities of long rows, or beside a score far above theirs, are below
+// the smallest normal number of fp16, 2^-14.  Backwards they are at most 1 and
+// taken times 2^15; forwards they are at most 2^slack, for a running maximum
+// that is taken `lift` below the largest score.  Score gradients have a range
+// of their own (value_magnitude_kernel).
 struct Fp16 {
     using raw = _Float16;
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
@@ -48,7 +50,7 @@ struct Fp16 {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
     static constexpr bool narrow = true;
-    static constexpr float p_gain = 64.0f, p_shift = 6.0f;
+    static constexpr float p_gain = 32768.0f, p_shift = 15.0f, lift = 11.0f, slack = 4.0f;
     static constexpr uint32_t exponent = 0x7C007C00u, least = 0x04000400u;
 };
 
@@ -629,10 +631,10 @@ __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
             for (int i = 1; i < 32; i++) most = fmaxf(most, x[i]);
             most = fmaf(fmaxf(most, other_half(most)), gain, offset);
             // The sums are moved to a new maximum only where the old one would let
-            // them grow by more than 2^8: 32-bit sums have room, and a probability
+            // them grow by more than 2^slack: 32-bit sums have room, and a probability
             // is rounded relative to itself.
-            if (__any(most > m + 8.0f)) {
-                const float m_new = fmaxf(m, most), f = exp2_(m - m_new);
+            if (__any(most > m + (T::lift + T::slack))) {
+                const float m_new = fmaxf(m, most - T::lift), f = exp2_(m - m_new);
                 m = m_new;
                 l *= f;
 #pragma unroll
@@ -803,8 +805,8 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(AttnArgs a)
 #pragma unroll
         for (int i = 1; i < 16; i++) most = fmaxf(most, x[i]);
         most = fmaxf(most, other_half(most)) * gain;
-        if (__any(most > m + 8.0f)) {                    // as in the forward kernel above
-            const float m_new = fmaxf(m, most), f = exp2_(m - m_new);
+        if (__any(most > m + (T::lift + T::slack))) {    // as in the forward kernel above
+            const float m_new = fmaxf(m, most - T::lift), f = exp2_(m - m_new);
             m = m_new;
             l *= f;
 #pragma unroll

@@ -1195,3 +1195,28 @@ def test_attention_contiguous_rows_at_odd_addresses(ops, shape):
     out = ops.attention(*ins, causal=True)
     for a, b in zip((out, *torch.autograd.grad(out, ins, odd(do))), want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("Sq", [1, 64])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("high", [9.0, 15.2, 19.0])
+def test_attention_small_probabilities_in_fp16(ops, Sq, D, high):
+    """Many keys beside one of a high score and no value: their probabilities are rounded by u = 2^-11 of themselves
+    and so is the output, though e^-19 is below fp16's range; two u are left for sums, score and exponential."""
+    Sk = 20000
+    q = torch.zeros(1, Sq, 1, D, device="cuda", dtype=FP)
+    k = torch.zeros(1, Sk, 1, D, device="cuda", dtype=FP)
+    v = torch.ones(1, Sk, 1, D, device="cuda", dtype=FP)
+    q[..., 0], k[:, 77, :, 0], v[:, 77] = high, 1.0, 0.0
+    do = torch.full_like(q, 1000.0)
+    score = float(q[0, 0, 0, 0])
+    small = math.exp(-score) / (1 + (Sk - 1) * math.exp(-score))
+    for t in (q, k, v):
+        t.requires_grad_()
+    out = ops.attention(q, k, v, scale=1.0)
+    want = (Sk - 1) * small
+    assert (out.double() - want).abs().max() <= 4 * U[FP] * want, (out.max().item(), out.min().item(), want)
+    dv, = torch.autograd.grad(out, v, do)
+    others = torch.arange(Sk, device="cuda") != 77
+    want = Sq * 1000.0 * small
+    assert (dv[:, others].double() - want).abs().max() <= 4 * U[FP] * want + 2 * TINY[FP], (dv[:, others].max().item(), want)
