@@ -1220,3 +1220,29 @@ def test_attention_small_probabilities_in_fp16(ops, Sq, D, high):
     others = torch.arange(Sk, device="cuda") != 77
     want = Sq * 1000.0 * small
     assert (dv[:, others].double() - want).abs().max() <= 4 * U[FP] * want + 2 * TINY[FP], (dv[:, others].max().item(), want)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_attention_training_step_in_a_graph(ops, dtype):
+    """Forward and backward pass captured, and replayed on other numbers with eager work in between."""
+    q, k, v, do = inputs(2, 200, 200, 4, 2, 64, dtype)
+    docs = (torch.arange(200)[None] // 70).expand(2, -1).to(torch.int32).cuda()
+
+    def step():
+        out = ops.attention(q, k, v, causal=True, docs=docs, cap=20.0)
+        return (out.detach(), *torch.autograd.grad(out, (q, k, v), do))
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(4):
+        with torch.no_grad():
+            for t in (q, k, v, do):
+                t.mul_(0.5 if i % 2 else -1.5)
+        want = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b), i
