@@ -49,7 +49,8 @@ extern "C" {
  * A query that sees no key has out = 0, lse = -infinity and adds nothing to
  * any gradient.  Sums and softmax statistics are held in 32 bits; the
  * probabilities (and, backward, the gradients of the scores) are rounded to
- * the inputs' type for the matrix instructions.
+ * the inputs' type for the matrix instructions, in fp16 times powers of two
+ * that keep them within its range.
  * Keys from lengths[b] on are not read (values there may be anything).
  * Infinities and NaN reach the queries that see them and no others.  Gradients
  * of a query that has an infinite component, or sees a key with one, may be

@@ -159,7 +159,8 @@ __device__ __forceinline__ float minus_half(float x2) { return __builtin_amdgcn_
 // 1.3e-7 cap whatever the score.  Up to 128 that is below a tenth of fp16's
 // unit (2^-12, as the probabilities are rounded); larger caps take the series
 // of tanh where scores are below a quarter of the cap, and keep the digits of
-// the score.
+// the score (8192 tokens in three documents, a whole pass: 1.62 ms, at a cap of
+// 50 1.29).
 enum { PLAIN = 0, SMALL = 1, LARGE = 2 };
 constexpr float LARGE_CAP = 128.0f;
 
@@ -531,13 +532,14 @@ template <int CAP> struct Shape {
 // its way from memory while one is worked on (two buffers, one barrier a
 // tile).  Rows are packed over the heads of a group, so that shared keys are
 // read once for all of them.
-//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 316 us, 0.87 PFLOP/s of
-// the visible half; a large product reaches 1.19 to 1.35 on this card.  The
-// rest is the softmax between the two products: the vector unit and the matrix
-// unit of a wavefront take turns, and two wavefronts a unit overlap in part.
-// With a cap the vector unit bounds it: three transcendental instructions a
-// score instead of one (8192 tokens in three documents, 16 heads over 4: 303
-// us, 0.45 PFLOP/s).
+//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 306 to 322 us, 0.87 PFLOP/s
+// of the visible half; a large product reaches 1.19 to 1.35 on this card.  No
+// unit is full: the matrix unit works in 42 % of the cycles, the vector unit
+// issues in 47 %.  A wavefront's products and its softmax take turns, and two
+// wavefronts a SIMD overlap in part.  With a cap, three transcendental
+// instructions a score instead of one (8192 tokens in three documents, 16 heads
+// over 4: 303 us, 0.45 PFLOP/s; 20 and 40 %, and a quarter of the card idle at
+// the end).
 
 template <typename T, int NB, bool SHAPED, int CAP>
 __global__ void __launch_bounds__(256, 2) forward_kernel(AttnArgs a)
@@ -938,6 +940,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a)
 // what its own rounding takes.  Here a workgroup finds the largest finite
 // number of its chunk of a unit's values; the gradients of rows that see
 // something are looked at by the kernel of dQ, for that of dK and dV too.
+//   4 x 4096 tokens, 16 heads of 128: 13 us (5.2 TB/s) beside 1500; 8 x 512 tokens, 12
+// heads of 64: 4.5 us beside 90.
 template <typename T>
 __global__ void __launch_bounds__(256) value_magnitude_kernel(AttnGradArgs a)
 {
@@ -996,9 +1000,10 @@ __device__ __forceinline__ int gradient_shift(int head_dim, float v, float dout)
 // product: dQ and dK are then up to 1.5 times as far from the exact gradient as
 // their own rounding makes them (0.0025 against 0.0017 of its norm in bf16).
 // The other way, dS in two parts, costs every such product twice.
-//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 430 us for three products
-// (0.96 PFLOP/s); 8192 tokens in three documents, capped: 387 us.  Bound by the
-// matrix unit, whose clock falls under load, and with a cap by the vector unit.
+//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 421 to 437 us for three
+// products (0.96 PFLOP/s; the matrix unit works in 48 % of the cycles, the
+// vector unit issues in 40 %, at a clock of 1.9 GHz under this load); 8192
+// tokens in three documents, capped: 380 to 395 us (25 and 39 %).
 // Two workgroups a compute unit, but for fp16's large caps at 128 columns: they
 // need 8 bytes a lane more than half of the registers.
 template <typename T, int NB, int CAP, bool BIAS>
@@ -1167,10 +1172,12 @@ __global__ void __launch_bounds__(256, CAP == LARGE && NB == 4 && T::narrow ? 1 
 // are added up by grad_join_kernel.  Keys and values stay in registers as
 // operands, dK and dV as accumulators: from 65 columns on one workgroup a
 // compute unit.
-//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 740 us for four products
-// (0.74 PFLOP/s; 690 where the clock is not yet down); 8192 tokens in three documents, 16 heads over 4, capped: 627
-// us and 33 for the join.  A cap and a bias are template arguments: with both tested in the loop
-// the accumulators moved between register files at every step.
+//   4 x 4096 tokens, 16 heads of 128, causal, bf16: 720 to 760 us for four
+// products (0.74 PFLOP/s; one wavefront a SIMD: the matrix unit works in 33 % of
+// the cycles, the vector unit issues in 27 %); 8192 tokens in three documents, 16
+// heads over 4, capped: 640 us (19 and 28 %) and 33 for the join.  A cap and a
+// bias are template arguments: with both tested in the loop the accumulators
+// moved between register files at every step.
 template <typename T, int NB, int CAP, bool BIAS>
 __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnGradArgs a)
 {
@@ -1449,6 +1456,11 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 1) dkv_kernel(AttnGradArgs 
         }
     };
     if constexpr (NB == 2) {
+        // One loop for up to 64 columns.  Two loops, as below, spill registers where
+        // there are a cap and a bias, and measured 324 us against 297 with a cap (8192
+        // tokens in three documents, 16 heads over 4), 43 against 40 with a bias and
+        // lengths (8 x 512 tokens, 12 heads), and without either 352 against 418 (4 x
+        // 4096 tokens, 16 heads, causal).
         walk(2, any_step);
     } else {
         // in loops of their own, or the sums would move between registers in every step

@@ -123,7 +123,9 @@ Plan make_plan(const dtr_attn *a, bool backward)
         p.parts = parts_for(units * ((a->k_len + GRAD_KEYS - 1) / GRAD_KEYS), rows);
         p.row_stat = take(sizeof(float2) * units * rows);
         if (a->type == DTR_FP16) {
-            // two workgroups a compute unit to read all of v
+            // two workgroups a compute unit to read all of v: 64 units of 4096 keys 13 us,
+            // 27 with a quarter of them and 13 with four times as many; 96 units of 512 keys
+            // 4.6, 6.5 and 5.4
             p.chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(units, 1), 64));
             p.value_magnitude = take(sizeof(float) * units * p.chunks);
             p.row_magnitude = take(sizeof(float) * units * ((rows + ROW_TILE - 1) / ROW_TILE) * 4);

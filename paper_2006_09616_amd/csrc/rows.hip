@@ -154,8 +154,8 @@ template <typename T> hipError_t dropout_typed(const DropArgs &a, hipStream_t st
 // (x - m) give lse = m + log l and entropy = log l - w / l (w and log l
 // in units of log 2, as the exponential instruction has it).  Bound by reading
 // the row: 4096 rows of 32000 in 16 bits, 52 us (5.0 TB/s); with 20
-// alternatives, whose vectors are read again, 8192 rows of 100003, 400-425 us
-// (4 TB/s); 4 rows of 50021 in 32 bits in 48 parts, 9 us and 4 for their join.
+// alternatives, whose vectors are read again, 8192 rows of 100003, 358-430 us
+// by the inputs (3.8 to 4.6 TB/s); 4 rows of 50021 in 32 bits in 48 parts, 9 us and 4 for their join.
 
 constexpr float LOWEST = -3.402823466e+38f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
